@@ -19,6 +19,7 @@
  *     values          [nnz]
  *   Dense matrices are row-major with no padding (leading dimension == number of columns).
  *   Sizes: m, k, n, nnz >= 0 and m*n, k*n < 2^31.  m == 0, n == 0 and nnz == 0 are valid.
+ *   (spdl_attention takes strides and 64-bit sizes.)
  *   Base pointers must be aligned to their element type.  The fast kernels take any alignment and
  *   any n from 4 on (fp16 on the matrix cores: 8); rows that are whole 16-byte pieces at 16-byte
  *   aligned addresses are the fastest, by a few percent in fp32 (n = 127: 95 us where n = 128
@@ -249,6 +250,80 @@ int spdl_build_row_order(int m, const int* row_offsets_host, int* row_order_host
  *   row_offsets_host : HOST int32[m+1];  column_indices_host : HOST int32[nnz]. */
 int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
                            const int* column_indices_host, int* sorted_out);
+
+/* Attention in one call: spdl_sddmm, spdl_csr_softmax and spdl_spmm of all heads of a layer (paper Sec. "Application: Sparse
+ * Transformer") in one pass that keeps no scores, of m queries to k states (their own, or an encoder's of another length), over
+ * the positions of a sparse matrix or all of them, with a learned bias by relative position, and the gradients of all of it.
+ * Query i of sequence b and head h sees state j where j < lengths[b] and, with a mask, where the m x k sparse matrix stores (i, j):
+ *   s_ij = scale * sum_c Q[b,h,i,c] K[b,g,j,c] + table[h, bucket_of[span + clamp(j - i - positions[b], -span, span)]]
+ *   lse[b,h,i] = log sum_j exp(s_ij),   P_ij = exp(s_ij - lse[b,h,i]),   O[b,h,i,:] = sum_j P_ij V[b,g,j,:]
+ * with g = h / (heads / kv_heads): consecutive query heads share a head of K and V.  A row that sees nothing, or whose scores are all
+ * -inf, has O = 0, lse = -inf and no part in any gradient.
+ *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads), 1 <= d <= 128
+ *     (SPDL_ERR_UNSUPPORTED above).  scale: finite.  span (0 .. 1024) and buckets (1 .. 128) are those of the bias.
+ *     Strides, in elements, of [batch, head, row] for each tensor; the d elements of a row lie next to one another.  Those of inputs
+ *     are >= 0 (0: the same for all); the elements of an output must not share addresses.  Only the strides of tensors that a
+ *     call takes are looked at.
+ *   Q, O, dO, dQ : DEVICE, [batch, heads, m, d].  K, V, dK, dV : DEVICE, [batch, kv_heads, k, d].  lse : DEVICE fp32[batch*heads*m];
+ *     may be NULL in the forward pass.  Base pointers are aligned to their element type; pieces of 16 bytes may start anywhere.
+ *   lengths : DEVICE int32[batch], how many states each sequence has (taken as 0 below 0, as k above k); NULL: k of each.  What lies
+ *     in K and V behind a sequence's states is not read.
+ *   mask : DEVICE, from spdl_build_attention_mask for this m and k; NULL: every position.  One for all sequences and heads.
+ *   bucket_of : DEVICE int32[2*span+1], each in [0, buckets) (spdl_build_relative_buckets_host);  table : DEVICE [heads*buckets].
+ *     Both NULL: no bias.  A bias of -inf hides a position.
+ *   positions : DEVICE int32[batch], the position of query 0 among the states (a decoding step's m newest of L: L - m); NULL: 0.
+ *   workspace : DEVICE, spdl_attention_workspace bytes, 16-byte aligned; NULL where that is 0.  Its content before a call does not
+ *     matter; calls that may run at the same time need one each.
+ * Products and sums: fp32 in the fp32 functions.  In the _f16 ones products of binary16 and fp32 sums; weights P, and dS in the
+ * gradients, are rounded to binary16 (taken times a power of two that keeps them in its range) before they are multiplied; results are
+ * rounded once.  Results do not depend on how the work is split between workgroups beyond the order of sums, and are deterministic.
+ * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once.  */
+typedef struct { int64_t batch, head, row; } spdl_strides;
+typedef struct {
+  int batch, heads, kv_heads;
+  int m, k, d;
+  int span, buckets;
+  float scale;
+  spdl_strides Q, K, V, O, dO, dQ, dK, dV;
+} spdl_attention_problem;
+
+int spdl_attention(const spdl_attention_problem* problem, const float* Q, const float* K, const float* V, const int* lengths,
+                   const int* positions, const void* mask, const int* bucket_of, const float* table, float* O, float* lse,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+int spdl_attention_f16(const spdl_attention_problem* problem, const uint16_t* Q, const uint16_t* K, const uint16_t* V,
+                       const int* lengths, const int* positions, const void* mask, const int* bucket_of, const uint16_t* table,
+                       uint16_t* O, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients of spdl_attention: of its inputs, given dO, that of O.  O and lse are the forward pass's, all else as it was there.
+ *   With D_i = dO_i . O_i and dS_ij = P_ij (dO_i . V_j - D_i):  dV_j = sum P_ij dO_i, dK_j = scale sum dS_ij Q_i (both over the
+ *   query heads that share state j as well), dQ_i = scale sum dS_ij K_j, dtable[h, b] = sum of dS_ij of head h in bucket b.
+ *   dQ, dK, dV : fully overwritten (rows behind a sequence's states: 0).  dtable : DEVICE [heads*buckets], fully overwritten; NULL:
+ *   not wanted.  workspace: spdl_attention_workspace(problem, elem_bytes, 1). */
+int spdl_attention_backward(const spdl_attention_problem* problem, const float* Q, const float* K, const float* V, const int* lengths,
+                            const int* positions, const void* mask, const int* bucket_of, const float* table, const float* O,
+                            const float* lse, const float* dO, float* dQ, float* dK, float* dV, float* dtable, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+int spdl_attention_backward_f16(const spdl_attention_problem* problem, const uint16_t* Q, const uint16_t* K, const uint16_t* V,
+                                const int* lengths, const int* positions, const void* mask, const int* bucket_of,
+                                const uint16_t* table, const uint16_t* O, const float* lse, const uint16_t* dO, uint16_t* dQ,
+                                uint16_t* dK, uint16_t* dV, uint16_t* dtable, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the forward pass, or with backward != 0 of both (elem_bytes: 2 or 4); negative: a status. */
+int64_t spdl_attention_workspace(const spdl_attention_problem* problem, int elem_bytes, int backward);
+
+/* The sparse matrix of an attention, from its CSR topology, in the form that spdl_attention reads: bits by rows and by columns, a
+ * quarter of a byte per position of the matrix.  Built once per topology.
+ *   row_offsets, column_indices : DEVICE, any order inside a row; a column that a row stores twice counts once.
+ *   mask : DEVICE, spdl_attention_mask_bytes(m, k) bytes, 8-byte aligned, fully overwritten.  (Negative bytes: a status.) */
+int64_t spdl_attention_mask_bytes(int m, int k);
+int spdl_build_attention_mask(int m, int k, int nnz, const int* row_offsets, const int* column_indices, void* mask, void* stream);
+
+/* Buckets of relative positions (state minus query) -max_distance .. max_distance, growing in width with the distance.  Pure host code.
+ *   bidirectional != 0: states behind the query use the upper half of the buckets; otherwise they are in bucket 0.
+ *   With s the buckets of a side (buckets / 2, or all) and e = s / 2, distance n is in bucket n below e, then in bucket
+ *   e + floor((s - e) log(n / e) / log(max_distance / e)), at most the side's last.  buckets up to 128, e >= 1, e < max_distance <= 1024.
+ *   bucket_of_host : HOST int32[2*max_distance+1], written: the bucket_of of spdl_attention with span = max_distance. */
+int spdl_build_relative_buckets_host(int buckets, int max_distance, int bidirectional, int* bucket_of_host);
 
 /* Kernel selection (paper Sec. "Experiments", first paragraph: tile sizes and vector widths
  * are picked from the problem shape).  spdl_select_* report what the dispatcher would launch for

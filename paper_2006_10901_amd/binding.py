@@ -26,6 +26,8 @@ EXPORTS = (
     "spdl_permute_values", "spdl_sddmm_scaled", "spdl_sddmm_scaled_f16",
     "spdl_sddmm_nt", "spdl_sddmm_nt_f16", "spdl_spmm_f16_i16", "spdl_sddmm_ordered",
     "spdl_spmm_banded", "spdl_sddmm_banded", "spdl_spmm_skewed", "spdl_sddmm_skewed",
+    "spdl_attention", "spdl_attention_f16", "spdl_attention_backward", "spdl_attention_backward_f16", "spdl_attention_workspace",
+    "spdl_attention_mask_bytes", "spdl_build_attention_mask", "spdl_build_relative_buckets_host",
 )
 
 
@@ -43,6 +45,15 @@ class LaunchInfo(ctypes.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class Strides(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("batch", "head", "row")]
+
+
+class AttentionProblem(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_int) for name in ("batch", "heads", "kv_heads", "m", "k", "d", "span", "buckets")] +
+                [("scale", ctypes.c_float)] + [(name, Strides) for name in ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV")])
+
+
 def lib():
     global _lib
     if _lib is None:
@@ -57,6 +68,8 @@ def lib():
         _lib = ctypes.CDLL(LIB_PATH)
         _lib.spdl_status_string.restype = ctypes.c_char_p
         _lib.spdl_variant_name.restype = ctypes.c_char_p
+        for name in ("spdl_attention_workspace", "spdl_attention_mask_bytes"):
+            getattr(_lib, name).restype = ctypes.c_int64
         for name in EXPORTS:
             getattr(_lib, name)            # raises AttributeError if a declared symbol is absent
     return _lib
@@ -99,7 +112,13 @@ _SIGNATURES = {
     "spdl_csr_softmax": "i:m i:nnz I:row_offsets F:logits f:scale F:probabilities",
     ("spdl_permute_values", 4): "i:nnz i:elem_bytes I:perm F:values F:out",
     ("spdl_permute_values", 2): "i:nnz i:elem_bytes I:perm H:values H:out",
+    "spdl_build_attention_mask": "i:m i:k i:nnz I:row_offsets I:column_indices B:mask",
 }
+for _name, _t in (("spdl_attention{}", "F"), ("spdl_attention{}_f16", "H")):
+    _inputs = (f"P:problem ~{_t}:Q ~{_t}:K ~{_t}:V ?I:lengths ?I:positions ?B:mask ?I:bucket_of ?{_t}:table ")
+    _SIGNATURES[_name.format("")] = _inputs + f"~{_t}:O ?F:lse ?W:workspace"
+    _SIGNATURES[_name.format("_backward")] = (_inputs + f"~{_t}:O F:lse ~{_t}:dO ~{_t}:dQ ~{_t}:dK ~{_t}:dV ?{_t}:dtable "
+                                              "?W:workspace")
 
 
 class _Calls(dict):
@@ -212,6 +231,88 @@ def spdl_permute_values(nnz, elem_bytes, perm, values, out, stream=None):
     if elem_bytes not in (2, 4):
         raise ValueError("elem_bytes must be 2 or 4")
     _call["spdl_permute_values", elem_bytes](nnz, elem_bytes, perm, values, out, stream)
+    return out
+
+
+def attention_problem(Q, K, V, O, scale, bucket_of=None, table=None, dO=None, dQ=None, dK=None, dV=None):
+    """The problem of a call, from its tensors: [batch, heads, rows, d], rows of d elements that lie next to one another."""
+    p = AttentionProblem()
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q and K must be [batch, heads, rows, d]")
+    p.batch, p.heads, p.m, p.d = Q.shape
+    p.kv_heads, p.k = K.shape[1:3]
+    p.scale = float(scale)
+    if (bucket_of is None) != (table is None):
+        raise ValueError("bucket_of and table belong together")
+    if table is not None:
+        if bucket_of.dim() != 1 or bucket_of.shape[0] % 2 == 0 or table.dim() != 2 or table.shape[0] != p.heads:
+            raise ValueError("bucket_of must be [2 span + 1] and table [heads, buckets]")
+        p.span, p.buckets = bucket_of.shape[0] // 2, table.shape[1]
+    query, key = (p.batch, p.heads, p.m, p.d), (p.batch, p.kv_heads, p.k, p.d)
+    for name, t, shape in (("Q", Q, query), ("K", K, key), ("V", V, key), ("O", O, query), ("dO", dO, query), ("dQ", dQ, query),
+                           ("dK", dK, key), ("dV", dV, key)):
+        if t is None:
+            continue
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
+        if p.d > 1 and t.stride(3) != 1:
+            raise ValueError(f"the elements of a row of {name} must lie next to one another")
+        # a dimension of one element has no stride that matters
+        setattr(p, name, Strides(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))))
+    return p
+
+
+def spdl_attention(problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, workspace, stream=None):
+    _call["spdl_attention"](problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, workspace, stream)
+    return O
+
+
+def spdl_attention_f16(problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, workspace, stream=None):
+    _call["spdl_attention_f16"](problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, workspace, stream)
+    return O
+
+
+def spdl_attention_backward(problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, dO, dQ, dK, dV, dtable,
+                            workspace, stream=None):
+    _call["spdl_attention_backward"](problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, dO, dQ, dK, dV,
+                                     dtable, workspace, stream)
+    return dQ, dK, dV, dtable
+
+
+def spdl_attention_backward_f16(problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, dO, dQ, dK, dV, dtable,
+                                workspace, stream=None):
+    _call["spdl_attention_backward_f16"](problem, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse, dO, dQ, dK, dV,
+                                         dtable, workspace, stream)
+    return dQ, dK, dV, dtable
+
+
+def _bytes(n, where):
+    if n < 0:
+        raise SpdlError(int(n), where)
+    return int(n)
+
+
+def spdl_attention_workspace(problem, elem_bytes, backward=False):
+    return _bytes(lib().spdl_attention_workspace(ctypes.byref(problem), int(elem_bytes), int(bool(backward))),
+                  "spdl_attention_workspace")
+
+
+def spdl_attention_mask_bytes(m, k):
+    return _bytes(lib().spdl_attention_mask_bytes(int(m), int(k)), "spdl_attention_mask_bytes")
+
+
+def spdl_build_attention_mask(m, k, nnz, row_offsets, column_indices, mask, stream=None):
+    if mask.numel() < spdl_attention_mask_bytes(m, k):
+        raise ValueError("mask is too short")
+    _call["spdl_build_attention_mask"](m, k, nnz, row_offsets, column_indices, mask, stream)
+    return mask
+
+
+def spdl_build_relative_buckets_host(buckets, max_distance, bidirectional):
+    """Returns bucket_of as a numpy int32 array of 2 max_distance + 1."""
+    out = np.empty(max(0, 2 * int(max_distance) + 1), dtype=np.int32)
+    _check(lib().spdl_build_relative_buckets_host(int(buckets), int(max_distance), int(bool(bidirectional)),
+                                                  out.ctypes.data_as(ctypes.c_void_p)), "spdl_build_relative_buckets_host")
     return out
 
 

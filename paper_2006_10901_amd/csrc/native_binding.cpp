@@ -5,12 +5,17 @@
 //
 // bind(address, where, signature) returns a callable for one C entry point.  `signature` has one
 // "kind:name" field per argument:  i = int,  f = float,  then tensors on the GPU by element type:
-// I = int32, S = int16, F = float32, H = float16; a '?' before the kind (e.g. "?I:row_order") also
+// I = int32, S = int16, F = float32, H = float16, B = bytes (uint8); a '?' before the kind (e.g. "?I:row_order") also
 // takes None.  The last argument is always the stream: None (the current one), a
 // torch.cuda.Stream or the handle as an int.
+//
+// The entry points of attention take a problem (P, a ctypes structure, whose bytes are the C one's), tensors that need not be contiguous
+// (a '~' before the kind: their sizes and strides have to be the problem's) and a workspace (W: its pointer, then its bytes).  Their
+// tensors lie on one device, and the current stream is that device's.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -18,9 +23,11 @@
 #include <string>
 #include <vector>
 
+#include "../../include/spdl.h"
+
 namespace {
 
-struct Argument { char kind; bool optional; std::string name; };
+struct Argument { char kind; bool optional; std::string name; bool strided = false; };
 
 struct Entry {
   void* address;
@@ -30,7 +37,7 @@ struct Entry {
 };
 
 // The C entry points' parameter classes before the stream: i = int, f = float, p = pointer.
-const char* const kForms[] = {"iiiipppppp", "iiiippppp", "iiiippppppip", "iippfp", "iippp"};
+const char* const kForms[] = {"iiiipppppp", "iiiippppp", "iiiippppppip", "iippfp", "iippp", "iiippp", "ppppppppppppl", "pppppppppppppppppl"};
 constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
 
 // Raised through a callback, so that the exception class lives in Python.
@@ -41,6 +48,8 @@ const char* dtype_name(char kind) {
     case 'I': return "torch.int32";
     case 'S': return "torch.int16";
     case 'F': return "torch.float32";
+    case 'B':
+    case 'W': return "torch.uint8";
     default: return "torch.float16";
   }
 }
@@ -50,6 +59,8 @@ at::ScalarType dtype_of(char kind) {
     case 'I': return at::kInt;
     case 'S': return at::kShort;
     case 'F': return at::kFloat;
+    case 'B':
+    case 'W': return at::kByte;
     default: return at::kHalf;
   }
 }
@@ -104,11 +115,55 @@ bool as_pointer(PyObject* o, const Argument& a, void** out) {
                  scalar_type_name(t.scalar_type()));
     return false;
   }
-  if (!t.is_contiguous()) {
+  if (!a.strided && !t.is_contiguous()) {
     PyErr_Format(PyExc_ValueError, "%s must be contiguous", a.name.c_str());
     return false;
   }
   *out = t.data_ptr();
+  return true;
+}
+
+// The bytes of a ctypes structure.
+bool as_problem(PyObject* o, const Argument& a, void** out) {
+  Py_buffer view;
+  if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) return false;
+  const bool ok = view.len == (Py_ssize_t)sizeof(spdl_attention_problem);
+  *out = view.buf;                                       // the caller holds the object for the length of the call
+  PyBuffer_Release(&view);
+  if (!ok) PyErr_Format(PyExc_ValueError, "%s must be an AttentionProblem", a.name.c_str());
+  return ok;
+}
+
+// Whether a tensor has the sizes and strides that the problem says it has.
+bool fits_problem(const at::Tensor& t, const Argument& a, const spdl_attention_problem& p) {
+  const std::string& n = a.name;
+  const bool keys = n == "K" || n == "V" || n == "dK" || n == "dV";
+  const spdl_strides& s = n == "Q" ? p.Q : n == "K" ? p.K : n == "V" ? p.V : n == "O" ? p.O : n == "dO" ? p.dO : n == "dQ" ? p.dQ : n == "dK" ? p.dK : p.dV;
+  const int64_t sizes[4] = {p.batch, keys ? p.kv_heads : p.heads, keys ? p.k : p.m, p.d}, strides[4] = {s.batch, s.head, s.row, 1};
+  bool ok = t.dim() == 4;
+  for (int i = 0; ok && i < 4; ++i) ok = t.size(i) == sizes[i] && (t.size(i) <= 1 || t.stride(i) == strides[i]);
+  if (!ok) PyErr_Format(PyExc_ValueError, "%s does not have the sizes and strides of the problem", n.c_str());
+  return ok;
+}
+
+// spdl_attention_mask_bytes: words by rows and by columns, and which tiles of them hold anything.
+int64_t mask_bytes(int64_t m, int64_t k) {
+  const int64_t ti = (m + 63) / 64, tj = (k + 63) / 64;
+  return 8 * (2 * 64 * ti * tj + ti * ((tj + 63) / 64) + tj * ((ti + 63) / 64));
+}
+
+// How many elements the problem has the arrays hold whose sizes are not their own.
+bool long_enough(const at::Tensor& t, const Argument& a, const spdl_attention_problem& p) {
+  int64_t needed = 0;
+  if (a.name == "lengths" || a.name == "positions") needed = p.batch;
+  else if (a.name == "bucket_of") needed = 2 * (int64_t)p.span + 1;
+  else if (a.name == "table" || a.name == "dtable") needed = (int64_t)p.heads * p.buckets;
+  else if (a.name == "lse") needed = (int64_t)p.batch * p.heads * p.m;
+  else if (a.name == "mask") needed = mask_bytes(p.m, p.k);
+  if (t.numel() < needed) {
+    PyErr_Format(PyExc_ValueError, "%s is too short", a.name.c_str());
+    return false;
+  }
   return true;
 }
 
@@ -135,7 +190,7 @@ bool as_stream(PyObject* o, void** out) {
   return true;
 }
 
-constexpr int kMaxArgs = 12;         // the longest of kForms
+constexpr int kMaxArgs = 20;         // the longest of kForms, the workspace counting twice
 
 PyObject* call_entry(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   const Entry& e = *static_cast<const Entry*>(PyCapsule_GetPointer(self, nullptr));
@@ -148,7 +203,10 @@ PyObject* call_entry(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   void* p[kMaxArgs];
   float f = 0.f;
   int ni = 0, np = 0, status = 0;
+  int64_t bytes = 0;
   void* st = nullptr;
+  const spdl_attention_problem* problem = nullptr;
+  c10::hip::OptionalHIPGuard guard;
   try {
     for (int a = 0; a < count; ++a) {
       const Argument& arg = e.args[a];
@@ -160,8 +218,21 @@ PyObject* call_entry(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
         const double v = PyFloat_AsDouble(args[a]);
         if (v == -1.0 && PyErr_Occurred()) return nullptr;
         f = (float)v;
+      } else if (arg.kind == 'P') {
+        if (!as_problem(args[a], arg, &p[np])) return nullptr;
+        problem = static_cast<const spdl_attention_problem*>(p[np++]);
       } else if (!as_pointer(args[a], arg, &p[np++])) {
         return nullptr;
+      } else if (problem && args[a] != Py_None) {
+        const at::Tensor& t = THPVariable_Unpack(args[a]);
+        if (arg.strided ? !fits_problem(t, arg, *problem) : !long_enough(t, arg, *problem)) return nullptr;
+        if (arg.kind == 'W') bytes = t.numel();
+        if (!guard.current_device()) {
+          guard.set_index(t.device().index());
+        } else if (t.device().index() != guard.current_device()->index()) {
+          PyErr_Format(PyExc_ValueError, "%s is on another device than the arguments before it", arg.name.c_str());
+          return nullptr;
+        }
       }
     }
     if (!as_stream(args[count], &st)) return nullptr;
@@ -187,8 +258,19 @@ PyObject* call_entry(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
     case 3:
       status = reinterpret_cast<int (*)(int, int, P, P, float, P, P)>(e.address)(i[0], i[1], p[0], p[1], f, p[2], st);
       break;
-    default:
+    case 4:
       status = reinterpret_cast<int (*)(int, int, P, P, P, P)>(e.address)(i[0], i[1], p[0], p[1], p[2], st);
+      break;
+    case 5:
+      status = reinterpret_cast<int (*)(int, int, int, P, P, P, P)>(e.address)(i[0], i[1], i[2], p[0], p[1], p[2], st);
+      break;
+    case 6:
+      status = reinterpret_cast<int (*)(P, P, P, P, P, P, P, P, P, P, P, P, int64_t, P)>(e.address)(
+          p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], bytes, st);
+      break;
+    default:
+      status = reinterpret_cast<int (*)(P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, int64_t, P)>(e.address)(
+          p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15], p[16], bytes, st);
   }
   Py_END_ALLOW_THREADS
   if (status != 0) {
@@ -219,9 +301,12 @@ PyObject* bind(PyObject*, PyObject* args) {
     Argument a;
     a.optional = s[at] == '?';
     if (a.optional) ++at;
+    a.strided = s[at] == '~';
+    if (a.strided) ++at;
     a.kind = s[at];
     a.name = s.substr(at + 2, end - at - 2);
     form += a.kind == 'i' || a.kind == 'f' ? a.kind : 'p';
+    if (a.kind == 'W') form += 'l';
     e->args.push_back(a);
     at = end + 1;
   }

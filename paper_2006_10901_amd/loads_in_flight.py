@@ -83,29 +83,33 @@ def hazards(lines, base=0):
 def disassembly(library, rocm="/opt/rocm"):
     """{kernel: (address, lines)} of the gfx950 code in a HIP library."""
     tools = os.path.join(rocm, "llvm", "bin")
+    magic, kernels = b"__CLANG_OFFLOAD_BUNDLE__", {}
     with tempfile.TemporaryDirectory() as tmp:
         bundle, obj = os.path.join(tmp, "bundle"), os.path.join(tmp, "obj")
         subprocess.run([os.path.join(tools, "llvm-objcopy"), "--dump-section", ".hip_fatbin=" + bundle, library, os.devnull],
                        check=True)
         data = open(bundle, "rb").read()
-        if not data.startswith(b"__CLANG_OFFLOAD_BUNDLE__"):
+        if not data.startswith(magic):
             raise RuntimeError(f"{library}: no code object bundle")
-        pos = 32
-        for _ in range(struct.unpack_from("<Q", data, 24)[0]):
-            start, size, length = struct.unpack_from("<QQQ", data, pos)
-            if b"gfx950" in data[pos + 24:pos + 24 + length]:
-                open(obj, "wb").write(data[start:start + size])
-            pos += 24 + length
-        text = subprocess.run([os.path.join(tools, "llvm-objdump"), "-d", "--mcpu=gfx950", obj], check=True,
-                              stdout=subprocess.PIPE, text=True).stdout
-    kernels, lines = {}, []
-    for line in text.splitlines():
-        head = re.match(r"([0-9a-f]+) <(.*)>:$", line)
-        if head:
+        first = 0
+        while first >= 0:                                 # one bundle per source file
+            pos = first + 32
+            for _ in range(struct.unpack_from("<Q", data, first + 24)[0]):
+                start, size, length = struct.unpack_from("<QQQ", data, pos)
+                if b"gfx950" in data[pos + 24:pos + 24 + length]:
+                    open(obj, "wb").write(data[first + start:first + start + size])
+                pos += 24 + length
+            text = subprocess.run([os.path.join(tools, "llvm-objdump"), "-d", "--mcpu=gfx950", obj], check=True,
+                                  stdout=subprocess.PIPE, text=True).stdout
             lines = []
-            kernels[head.group(2)] = (int(head.group(1), 16), lines)
-        else:
-            lines.append(line)
+            for line in text.splitlines():
+                head = re.match(r"([0-9a-f]+) <(.*)>:$", line)
+                if head:
+                    lines = []
+                    kernels[head.group(2)] = (int(head.group(1), 16), lines)
+                else:
+                    lines.append(line)
+            first = data.find(magic, first + 1)
     return kernels
 
 
