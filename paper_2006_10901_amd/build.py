@@ -6,6 +6,7 @@ import glob
 import os
 import shutil
 import subprocess
+import tempfile
 
 from . import loads_in_flight
 
@@ -20,6 +21,10 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]
+
+# The attention kernels: results of matrix instructions in ordinary vector registers.  Left to itself the compiler keeps them in the
+# accumulation registers, which no other instruction takes, and moves each score there and back (64 to 96 moves per tile).
+SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 MICROBENCH_SRC = os.path.join(_HERE, "microbench", "inner_loop_rates.hip")
@@ -45,13 +50,8 @@ CLOCKS_LIB_PATH = os.path.join(_HERE, "microbench", "libspdl_phase_clocks.so")
 def build_phase_clocks(verbose: bool = False) -> str:
     """A second copy of the library with clocks compiled into the slab kernels
     (-DSPDL_PHASE_CLOCKS), for microbench/phase_clocks.py only; the product library has none."""
-    cmd = [HIPCC, *HIP_FLAGS, "-DSPDL_PHASE_CLOCKS", "-o", CLOCKS_LIB_PATH, *sources()]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + proc.stdout)
-    return CLOCKS_LIB_PATH
+    return _compile_and_link(CLOCKS_LIB_PATH, ["-DSPDL_PHASE_CLOCKS"], [s for s in sources() if os.path.basename(s) not in SOURCE_FLAGS],
+                             verbose)
 
 
 NATIVE_PATH = os.path.join(_HERE, "_native.so")
@@ -78,14 +78,29 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
+def _compile_and_link(library, flags, files, verbose):
+    """One object per source file, compiled side by side, then the library."""
+    compile_flags = [f for f in HIP_FLAGS if f != "-shared"] + flags
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in files]
+        cmds = [[HIPCC, *compile_flags, *SOURCE_FLAGS.get(os.path.basename(s), []), "-c", "-o", o, s] for s, o in zip(files, objects)]
+        running = []
+        for cmd in cmds:
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        for proc, output in [(p, p.communicate()[0]) for p in running]:
+            if proc.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + output)
+        proc = subprocess.run([HIPCC, *HIP_FLAGS, "-o", library, *objects], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if proc.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + proc.stdout)
+    return library
+
+
 def build_library(verbose: bool = False) -> str:
     """The C library alone: needs hipcc, neither torch nor g++."""
-    cmd = [HIPCC, *HIP_FLAGS, "-o", LIB_PATH, *sources()]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + proc.stdout)
+    _compile_and_link(LIB_PATH, [], sources(), verbose)
     loads_in_flight.check(LIB_PATH, os.path.dirname(os.path.dirname(shutil.which(HIPCC) or HIPCC)))
     return LIB_PATH
 

@@ -21,13 +21,26 @@ struct Plan {
   int forward_splits, dq_splits, dkv_splits;
   int64_t forward_blocks, dq_blocks, dkv_blocks;      // without the splits
   int64_t rows, kv_rows, parts;        // parts: workgroups that leave sums of dS per head
-  // offsets into the workspace, in bytes
-  int64_t part_lse, forward_bytes;
-  int64_t delta, part, part_bias, backward_bytes;
+  int width;                           // d rounded up to the width of a kernel
+  bool copied;                         // whether the panel kernels take copies of Q, K, V and dO: fp16 terms of fp32 numbers, or rows
+                                       // of whole 16-byte pieces where the caller's are not
+  int most_parts;
+  // offsets into the workspace, in bytes; the terms of Q, K, V and dO and their factors come first (single precision)
+  int64_t most, factors, q16, k16, v16, g16;
+  int64_t forward_part, part_lse, forward_bytes;
+  int64_t delta, part, row_sums, part_bias, backward_bytes;
 };
+
+inline int kernel_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 
 inline int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 inline int64_t room(int64_t floats) { return up(floats * 4, 256) * 256; }
+// Takes room for `floats` at the end of a layout.
+inline int64_t take(int64_t& end, int64_t floats) {
+  const int64_t at = end;
+  end += room(floats);
+  return at;
+}
 
 // How many workgroups a panel's work is split over: enough to give every compute unit `want` of them, of at least `least` steps each.
 inline int split_count(int64_t blocks, int64_t steps, int want, int least) {
@@ -36,11 +49,12 @@ inline int split_count(int64_t blocks, int64_t steps, int want, int least) {
   return (int)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
 
-Plan make_plan(const spdl_attention_problem& p) {
+Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   Plan x{};
   const int64_t group = p.kv_heads ? p.heads / p.kv_heads : 1;
   x.rows = (int64_t)p.batch * p.heads * p.m;
   x.kv_rows = (int64_t)p.batch * p.kv_heads * p.k;
+  x.width = kernel_width(p.d);
   x.token = p.m <= 16;
   if (x.token) {
     x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, 32);
@@ -53,13 +67,34 @@ Plan make_plan(const spdl_attention_problem& p) {
   x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, 4);
   x.dkv_blocks = (int64_t)p.batch * p.kv_heads * up(p.k, kAttnPanel);
   x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, 4);
-  x.part_lse = x.forward_splits > 1 ? room(x.forward_splits * x.rows * p.d) : 0;
-  x.forward_bytes = x.forward_splits > 1 ? x.part_lse + room(x.forward_splits * x.rows) : 0;
-  x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dq_splits;
-  x.delta = 0;
-  x.part = room(x.rows);
-  x.part_bias = x.part + room(std::max(x.dq_splits > 1 ? x.dq_splits * x.rows * p.d : 0, x.dkv_splits > 1 ? 2 * x.dkv_splits * x.kv_rows * p.d : 0));
-  x.backward_bytes = x.part_bias + (p.buckets > 0 ? room(x.parts * p.heads * (2 * (int64_t)p.span + 1)) : 0);
+  x.parts = (int64_t)p.batch * up(p.m, kAttnPanel);
+  x.most_parts = (int)std::min<int64_t>(64, std::max<int64_t>(1, up(std::max<int64_t>(group * p.m, p.k), 64)));
+
+  int64_t terms = 0, end = 0;
+  x.copied = elem_bytes == 4 || p.d % 8 != 0;
+  const int numbers = elem_bytes == 4 ? x.width : x.width / 2;    // floats' room that a row of terms takes
+  if (x.copied) {
+    x.most = take(terms, (int64_t)p.batch * p.kv_heads * 4 * x.most_parts);
+    x.factors = take(terms, (int64_t)p.batch * p.kv_heads * 4);
+    x.q16 = take(terms, x.rows * numbers);
+    x.k16 = take(terms, x.kv_rows * numbers);
+    x.v16 = take(terms, x.kv_rows * numbers);
+  }
+  end = x.token ? 0 : terms;
+  if (x.forward_splits > 1) {
+    x.forward_part = take(end, x.forward_splits * x.rows * p.d);
+    x.part_lse = take(end, x.forward_splits * x.rows);
+  }
+  x.forward_bytes = end;
+  end = terms;
+  if (x.copied) x.g16 = take(end, x.rows * numbers);
+  x.delta = take(end, x.rows);
+  x.part = take(end, std::max(x.dq_splits > 1 ? x.dq_splits * x.rows * p.d : 0, x.dkv_splits > 1 ? 2 * x.dkv_splits * x.kv_rows * p.d : 0));
+  if (p.buckets > 0) {
+    x.row_sums = take(end, 2 * x.dq_splits * x.rows * 5);
+    x.part_bias = take(end, x.parts * p.heads * (2 * (int64_t)p.span + 1));
+  }
+  x.backward_bytes = end;
   return x;
 }
 
@@ -122,41 +157,83 @@ bool launch(void (*kernel)(AttnArgs), int64_t blocks, int lds, const AttnArgs& a
   return hipGetLastError() == hipSuccess;
 }
 
+// The operands as the panel kernels take them: the caller's arrays in half precision; in single precision their terms, made here.
+template <typename T, int D>
+bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStream_t stream) {
+  if (!x.copied) {
+    a.q16 = static_cast<const _Float16*>(a.Q), a.q16s = a.q;
+    a.k16 = static_cast<const _Float16*>(a.K), a.k16s = a.kk;
+    a.v16 = static_cast<const _Float16*>(a.V), a.v16s = a.v;
+    a.g16 = static_cast<const _Float16*>(a.dO), a.g16s = a.dout;
+    a.width = a.d;
+    return true;
+  }
+  constexpr int kWidth = attn_terms<T>() * D;
+  AttnOperands o{};
+  auto operand = [&](const void* from, const AttnStrides& s, int64_t to, int group, int rows, int keys, const _Float16*& terms, AttnStrides& strides) {
+    _Float16* at = reinterpret_cast<_Float16*>(w + to);
+    o.of[o.count++] = {from, at, s, a.kv_heads, group, rows, keys};
+    terms = at;
+    strides = {(int64_t)a.kv_heads * group * rows * kWidth, (int64_t)rows * kWidth, kWidth};
+  };
+  operand(a.Q, a.q, x.q16, a.group, a.m, 0, a.q16, a.q16s);
+  operand(a.K, a.kk, x.k16, 1, a.k, 1, a.k16, a.k16s);
+  operand(a.V, a.v, x.v16, 1, a.k, 1, a.v16, a.v16s);
+  if (backward) operand(a.dO, a.dout, x.g16, a.group, a.m, 0, a.g16, a.g16s);
+  a.width = kWidth;
+  a.factors = reinterpret_cast<float*>(w + x.factors);
+  o.batch = a.batch, o.kv_heads = a.kv_heads, o.d = a.d, o.k = a.k, o.parts = x.most_parts, o.lengths = a.lengths;
+  o.most = reinterpret_cast<float*>(w + x.most), o.factors = reinterpret_cast<float*>(w + x.factors);
+  const int64_t each = (int64_t)a.batch * a.kv_heads * o.count;
+  if (sizeof(T) == 4) {
+    attention_largest_kernel<<<dim3((unsigned)(each * o.parts)), dim3(256), 0, stream>>>(o);
+    if (hipGetLastError() != hipSuccess) return false;
+  }
+  const int64_t blocks = up(std::max<int64_t>((int64_t)a.group * a.m, a.k), 256 / (D / 8));
+  attention_terms_kernel<T, D><<<dim3((unsigned)(each * blocks)), dim3(256), 0, stream>>>(o, blocks);
+  return hipGetLastError() == hipSuccess;
+}
+
 template <typename T, int D, bool BIAS>
-bool launch_forward(const Plan& x, const AttnArgs& a, hipStream_t stream) {
-  constexpr int kPitch = AttnTile<T, D>::kPitch;
+bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   if (x.token) {
-    const int lds = kAttnWaves * 2 * 32 * kPitch + (BIAS ? std::min(a.group, 32) * a.buckets * 4 + (2 * a.span + 1) * 4 : 0);
+    const int lds = kAttnWaves * 2 * 32 * TokenTile<T, D>::kPitch + (BIAS ? std::min(a.group, 32) * a.buckets * 4 + (2 * a.span + 1) * 4 : 0);
     return launch(attention_token_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream);
   }
-  const int lds = 2 * kAttnTile * kPitch + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
+  if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
+  using Tile = AttnTile<D, attn_terms<T>()>;
+  const int lds = Tile::kSets * Tile::kPair + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
   return launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream);
 }
 
 template <typename T, int D, bool BIAS>
-bool launch_backward(const Plan& x, AttnArgs a, float* part, hipStream_t stream) {
-  constexpr int kTiles = 2 * kAttnTile * AttnTile<T, D>::kPitch;
-  a.part = part;
-  const int64_t vec = (int64_t)a.d;
+bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
+  using Tile = AttnTile<D, attn_terms<T>()>;
+  constexpr int kTiles = Tile::kSets * Tile::kPair;
+  const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
+  float* part = a.part = reinterpret_cast<float*>(w + x.part);
+  if ((x.dq_blocks > 0 || x.dkv_blocks > 0) && !prepare_operands<T, D>(x, a, w, true, stream)) return false;
   if (x.dq_blocks > 0) {
     a.splits = x.dq_splits;
-    const int lds = kTiles + (BIAS ? attn_bias_entries(a.span) * 4 : 0) +
-                    (BIAS && a.part_bias ? kAttnWaves * (kAttnDiagBytes + (2 * a.span + 1) * 4) : 0);
-    if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, lds, a, stream)) return false;
+    if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, kTiles + bias, a, stream)) return false;
     if (a.splits > 1) {
-      attention_sum_kernel<T><<<dim3((unsigned)up(x.rows * vec, 256)), dim3(256), 0, stream>>>(a.splits, x.rows, a.heads, a.m, a.d, part, a.dq,
-                                                                                              static_cast<T*>(a.dQ));
+      attention_sum_kernel<T><<<dim3((unsigned)up(x.rows * a.d, 256)), dim3(256), 0, stream>>>(a.splits, x.rows, a.heads, a.m, a.d, part,
+                                                                                              AttnSum{a.dq, a.dQ}, AttnSum{});
       if (hipGetLastError() != hipSuccess) return false;
+    }
+    if (BIAS && a.part_bias) {
+      a.row_splits = a.splits;
+      a.splits = 1;
+      const int lds = kTiles + bias + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
+      if (!launch(attention_dbias_kernel<T, D>, x.dq_blocks, lds, a, stream)) return false;
     }
   }
   if (x.dkv_blocks > 0) {
     a.splits = x.dkv_splits;
-    const int lds = kTiles + 2 * kAttnTile * 4 + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
-    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, lds, a, stream)) return false;
-    for (int which = 0; which < 2 && a.splits > 1; ++which) {
-      attention_sum_kernel<T><<<dim3((unsigned)up(x.kv_rows * vec, 256)), dim3(256), 0, stream>>>(
-          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part + which * a.splits * x.kv_rows * vec, which ? a.dv : a.dk,
-          static_cast<T*>(which ? a.dV : a.dK));
+    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 2 * kAttnTile * 4 + bias, a, stream)) return false;
+    if (a.splits > 1) {
+      attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * a.d, 256)), dim3(256), 0, stream>>>(
+          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
       if (hipGetLastError() != hipSuccess) return false;
     }
   }
@@ -164,19 +241,19 @@ bool launch_backward(const Plan& x, AttnArgs a, float* part, hipStream_t stream)
 }
 
 template <typename T, bool BIAS>
-bool dispatch_forward(const Plan& x, const AttnArgs& a, hipStream_t stream) {
-  if (a.d <= 32) return launch_forward<T, 32, BIAS>(x, a, stream);
-  if (a.d <= 64) return launch_forward<T, 64, BIAS>(x, a, stream);
-  if (a.d <= 96) return launch_forward<T, 96, BIAS>(x, a, stream);
-  return launch_forward<T, 128, BIAS>(x, a, stream);
+bool dispatch_forward(const Plan& x, const AttnArgs& a, char* w, hipStream_t stream) {
+  if (a.d <= 32) return launch_forward<T, 32, BIAS>(x, a, w, stream);
+  if (a.d <= 64) return launch_forward<T, 64, BIAS>(x, a, w, stream);
+  if (a.d <= 96) return launch_forward<T, 96, BIAS>(x, a, w, stream);
+  return launch_forward<T, 128, BIAS>(x, a, w, stream);
 }
 
 template <typename T, bool BIAS>
-bool dispatch_backward(const Plan& x, const AttnArgs& a, float* part, hipStream_t stream) {
-  if (a.d <= 32) return launch_backward<T, 32, BIAS>(x, a, part, stream);
-  if (a.d <= 64) return launch_backward<T, 64, BIAS>(x, a, part, stream);
-  if (a.d <= 96) return launch_backward<T, 96, BIAS>(x, a, part, stream);
-  return launch_backward<T, 128, BIAS>(x, a, part, stream);
+bool dispatch_backward(const Plan& x, const AttnArgs& a, char* w, hipStream_t stream) {
+  if (a.d <= 32) return launch_backward<T, 32, BIAS>(x, a, w, stream);
+  if (a.d <= 64) return launch_backward<T, 64, BIAS>(x, a, w, stream);
+  if (a.d <= 96) return launch_backward<T, 96, BIAS>(x, a, w, stream);
+  return launch_backward<T, 128, BIAS>(x, a, w, stream);
 }
 
 inline bool workspace_ok(const void* workspace, int64_t bytes, int64_t needed) {
@@ -192,15 +269,16 @@ int attention(const spdl_attention_problem* p, const void* Q, const void* K, con
   if (!output_strides_ok(p->O, p->batch, p->heads, p->m, p->d)) return SPDL_ERR_INVALID;
   if (p->batch == 0 || p->heads == 0 || p->m == 0) return SPDL_OK;
   if (!Q || !O || (p->k > 0 && (!K || !V))) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p);
+  const Plan x = make_plan(*p, sizeof(T));
   if (!workspace_ok(workspace, workspace_bytes, x.forward_bytes)) return SPDL_ERR_INVALID;
   AttnArgs a = make_args(*p, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse);
   a.splits = x.forward_splits;
-  a.part = static_cast<float*>(workspace);
-  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + x.part_lse);
+  char* w = static_cast<char*>(workspace);
+  a.part = reinterpret_cast<float*>(w + x.forward_part);
+  a.part_lse = reinterpret_cast<float*>(w + x.part_lse);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (!(table ? dispatch_forward<T, true>(x, a, s) : dispatch_forward<T, false>(x, a, s))) return SPDL_ERR_LAUNCH;
+  if (!(table ? dispatch_forward<T, true>(x, a, w, s) : dispatch_forward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (a.splits > 1) {
     attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 4)), dim3(256), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
@@ -223,19 +301,19 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   const bool queries = p->batch > 0 && p->m > 0, keys = p->batch > 0 && p->k > 0;
   if (queries && (!Q || !O || !lse || !dO || !dQ)) return SPDL_ERR_INVALID;
   if (keys && (!K || !V || !dK || !dV)) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p);
+  const Plan x = make_plan(*p, sizeof(T));
   if ((queries || keys) && !workspace_ok(workspace, workspace_bytes, x.backward_bytes)) return SPDL_ERR_INVALID;
   AttnArgs a = make_args(*p, Q, K, V, lengths, positions, mask, bucket_of, table, const_cast<void*>(O), const_cast<float*>(lse));
   a.dO = dO, a.dQ = dQ, a.dK = dK, a.dV = dV;
   char* w = static_cast<char*>(workspace);
   a.delta = reinterpret_cast<float*>(w + x.delta);
+  a.row_sums = dtable ? reinterpret_cast<double*>(w + x.row_sums) : nullptr;
   a.part_bias = dtable ? reinterpret_cast<float*>(w + x.part_bias) : nullptr;
-  float* part = reinterpret_cast<float*>(w + x.part);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (!(table ? dispatch_backward<T, true>(x, a, part, s) : dispatch_backward<T, false>(x, a, part, s))) return SPDL_ERR_LAUNCH;
+  if (!(table ? dispatch_backward<T, true>(x, a, w, s) : dispatch_backward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (dtable) {
-    attention_dtable_kernel<T><<<dim3((unsigned)p->heads), dim3(1024), (2 * p->span + 1) * 4, s>>>(a, (int)x.parts, static_cast<T*>(dtable));
+    attention_dtable_kernel<T><<<dim3((unsigned)p->heads), dim3(1024), (2 * p->span + 1) * 12, s>>>(a, (int)x.parts, static_cast<T*>(dtable));
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   }
   return SPDL_OK;
@@ -247,7 +325,7 @@ extern "C" {
 
 int64_t spdl_attention_workspace(const spdl_attention_problem* p, int elem_bytes, int backward) {
   if (!p || !sizes_ok(*p) || p->d > kMostWidth || (elem_bytes != 2 && elem_bytes != 4)) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p);
+  const Plan x = make_plan(*p, elem_bytes);
   return backward ? std::max(x.forward_bytes, x.backward_bytes) : x.forward_bytes;
 }
 
@@ -293,7 +371,11 @@ int spdl_build_attention_mask(int m, int k, int nnz, const int* row_offsets, con
   attention_mask_clear_kernel<<<dim3((unsigned)up(words, 256)), dim3(256), 0, s>>>(words, static_cast<uint64_t*>(mask));
   if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   if (nnz == 0) return SPDL_OK;
-  attention_mask_kernel<<<dim3((unsigned)up(m, 4)), dim3(256), 0, s>>>(m, k, row_offsets, column_indices, static_cast<unsigned long long*>(mask));
+  auto* bits = static_cast<unsigned long long*>(mask);
+  attention_mask_rows_kernel<<<dim3((unsigned)up(m, 4)), dim3(256), 0, s>>>(m, k, row_offsets, column_indices, bits);
+  if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
+  const int64_t tiles = up(m, 64) * up(k, 64);
+  attention_mask_tiles_kernel<<<dim3((unsigned)up(tiles, 4)), dim3(256), 0, s>>>(m, k, bits);
   return hipGetLastError() == hipSuccess ? SPDL_OK : SPDL_ERR_LAUNCH;
 }
 

@@ -10,8 +10,12 @@
 //   operand is read from LDS in the order in which the registers hold the right one.
 //
 // The softmax needs the maximum of a column, which lies in lanes l and l + 32: one exchange per tile.  Statistics of a row are one number
-// per lane.  Half precision: products on 32 x 32 x 16 fp16 instructions, left operands of the second kind by LDS reads that transpose.
-// Single precision: 32 x 32 x 2 fp32 instructions.  All sums, the scores and their statistics are fp32.
+// per lane.  Left operands of the second kind come from LDS reads that transpose.  All sums, the scores and their statistics are fp32.
+//
+// Single precision: fp32 instructions do a sixteenth of the fp16 ones' work in the same time, so a number is two fp16 terms, taken times
+// a power of two that brings the largest of its head (all heads of a group) to 2^14 .. 2^15.  Two terms hold a number to 2^-23 of itself, or to
+// 2^-39 of the largest if that is more.  Of the four products of terms the smallest, below 2^-22 of the whole, is left out.
+// The terms are made once per call, by two small kernels, rather than by every workgroup that reads them.
 #pragma once
 #include "common.hpp"
 
@@ -33,10 +37,16 @@ struct AttnStrides { int64_t batch, head, row; };
 // What a call hands to the kernels.  mask_*: bits of the sparse matrix (see MaskLayout).
 struct AttnArgs {
   int batch, heads, kv_heads, group, m, k, d;
-  int span, buckets, splits;
+  int span, buckets, splits, row_splits;
   float scale;
   AttnStrides q, kk, v, o, dout, dq, dk, dv;
   const void *Q, *K, *V, *dO;
+  // The operands as fp16 terms, `width` of them per row: the caller's arrays in half precision, else arrays of two terms per number,
+  // and what the numbers of the sequence's (kv) heads were multiplied by, four factors for each: Q, K, V, dO
+  const _Float16 *q16, *k16, *v16, *g16;
+  AttnStrides q16s, k16s, v16s, g16s;
+  int width;
+  const float* factors;
   const int *lengths, *positions, *bucket_of;
   const void* table;
   const uint64_t* mask;
@@ -46,7 +56,8 @@ struct AttnArgs {
   float* delta;          // workspace, [batch, heads, m]
   float* part;           // workspace: what splits leave for the join
   float* part_lse;
-  float* part_bias;      // workspace: sums of dS by relative position, one set of 2 span + 1 per workgroup
+  double* row_sums;      // workspace: of every row and split, sums that the gradient of the bias needs (see attention_dq_kernel)
+  float* part_bias;      // workspace: sums of dS by relative position, one set of 2 span + 1 per panel
 };
 
 // The sparse matrix as bits, in words of 64: for every tile of 64 columns a word per row (row_words), for every tile of 64 rows a word
@@ -65,36 +76,27 @@ struct MaskLayout {
   }
 };
 
-template <typename T> struct AttnType;
-template <> struct AttnType<_Float16> {
-  typedef f16x8 Piece;                                   // 16 bytes
-  typedef f16x8 PieceAny __attribute__((aligned(2)));
-  // Weights are taken times 2^14: they are at most 1, and fp16 then holds those down to 2^-28 of the largest with all its bits and down
-  // to 2^-39 with some (as they are: 2^-14 and 2^-25, and a row of 2^16 even weights would lose most of its bits).
-  static constexpr float kOffset = 14.f;
-};
-template <> struct AttnType<float> {
-  typedef f32x4 Piece;
-  typedef f32x4 PieceAny __attribute__((aligned(4)));
-  static constexpr float kOffset = 0.f;
-};
+// Weights are taken times 2^14: they are at most 1, and fp16 then holds those down to 2^-28 of the largest with all its bits and down to
+// 2^-39 with some (as they are: 2^-14 and 2^-25, and a row of 2^16 even weights would lose most of its bits).
+constexpr float kOffset = 14.f;
 
-// Rows of D elements in LDS, 16 bytes apart from a multiple of the banks: lanes that read 16 bytes of 32 rows meet no conflict.
-template <typename T, int D> struct AttnTile {
-  static constexpr int kPiece = 16 / sizeof(T);          // elements per piece
-  static constexpr int kPieces = D / kPiece;             // pieces per row
-  static constexpr int kPitch = D * (int)sizeof(T) + 16; // bytes per row
-  static constexpr int kSteps = D * (int)sizeof(T) / 32; // pieces per row and half of the wave
+template <typename T> struct AttnPiece;                  // 16 bytes, and the same at any address of an element
+template <> struct AttnPiece<_Float16> {
+  typedef f16x8 Type;
+  typedef f16x8 Any __attribute__((aligned(2)));
+};
+template <> struct AttnPiece<float> {
+  typedef f32x4 Type;
+  typedef f32x4 Any __attribute__((aligned(4)));
 };
 
 // 16 bytes of a row of d elements, zeros from d on.
 template <typename T>
-__device__ __forceinline__ typename AttnType<T>::Piece attn_load_piece(const T* row, int c0, int d) {
-  using Piece = typename AttnType<T>::Piece;
+__device__ __forceinline__ typename AttnPiece<T>::Type attn_load_piece(const T* row, int c0, int d) {
   constexpr int E = 16 / sizeof(T);
-  Piece v = {};
+  typename AttnPiece<T>::Type v = {};
   if (c0 + E <= d) {
-    v = *reinterpret_cast<const typename AttnType<T>::PieceAny*>(row + c0);
+    v = *reinterpret_cast<const typename AttnPiece<T>::Any*>(row + c0);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -102,102 +104,154 @@ __device__ __forceinline__ typename AttnType<T>::Piece attn_load_piece(const T* 
   }
   return v;
 }
+// The same for rows of whole pieces, without a branch: pieces that are not wanted read one that is there.
+template <typename T>
+__device__ __forceinline__ typename AttnPiece<T>::Type attn_load_whole_piece(const T* row, int c0, int d, bool wanted) {
+  const typename AttnPiece<T>::Type v = *reinterpret_cast<const typename AttnPiece<T>::Any*>(row + min(c0, d - 16 / (int)sizeof(T)));
+  return wanted && c0 < d ? v : typename AttnPiece<T>::Type{};
+}
 
-// A tile on its way from memory to LDS: requested a tile ahead into registers, then written.
-template <typename T, int D, int ROWS, int THREADS> struct AttnStage {
-  using Tile = AttnTile<T, D>;
-  static constexpr int kCount = ROWS * Tile::kPieces / THREADS;
-  static_assert(ROWS * Tile::kPieces % THREADS == 0, "whole pieces per thread");
-  typename AttnType<T>::Piece v[kCount];
-  // rows [0, rows) of `base`, `stride` elements apart; zeros behind them
+// A tile on its way from memory to LDS, requested a tile ahead into registers, then written: ROWS rows of BYTES bytes, PITCH apart.
+template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnStage {
+  using Piece = typename AttnPiece<T>::Type;
+  static constexpr int kElements = 16 / (int)sizeof(T), kPieces = BYTES / 16, kCount = ROWS * kPieces / THREADS;
+  static_assert(ROWS * kPieces % THREADS == 0, "whole pieces per thread");
+  Piece v[kCount];
+  // rows [0, rows) of `base`, `stride` elements apart, of d elements, a multiple of a piece's; zeros behind them (rows >= 1)
   __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d, int tid) {
+    if (rows >= ROWS && d * (int)sizeof(T) == BYTES) {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) {
+        const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
+        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(base + row * stride + c * kElements);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) {
+        const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
+        v[i] = attn_load_whole_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d, row < rows);
+      }
+    }
+  }
+  // the same for any d
+  __device__ __forceinline__ void load_any(const T* base, int64_t stride, int rows, int d, int tid) {
+    if (d % kElements == 0) return load(base, stride, rows, d, tid);
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      const int at = i * THREADS + tid, row = at / Tile::kPieces, c = at % Tile::kPieces;
-      v[i] = typename AttnType<T>::Piece{};
-      if (row < rows) v[i] = attn_load_piece<T>(base + (int64_t)row * stride, c * Tile::kPiece, d);
+      const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
+      v[i] = Piece{};
+      if (row < rows) v[i] = attn_load_piece<T>(base + row * stride, c * kElements, d);
     }
   }
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      const int at = i * THREADS + tid, row = at / Tile::kPieces, c = at % Tile::kPieces;
-      *reinterpret_cast<typename AttnType<T>::Piece*>(lds + row * Tile::kPitch + c * 16) = v[i];
+      const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
+      *reinterpret_cast<Piece*>(lds + row * PITCH + c * 16) = v[i];
     }
   }
 };
 
-template <typename T, int D> using AttnOwn = typename AttnType<T>::Piece[AttnTile<T, D>::kSteps];
-
+// Rows of D numbers of TERMS fp16 terms each, the first terms of all, then the second.  In LDS 16 bytes apart from a multiple of the
+// banks: lanes that read 16 bytes of 32 rows meet no conflict.
+template <int D, int TERMS> struct AttnTile {
+  static constexpr int kBytes = D * TERMS * 2, kPitch = kBytes + 16, kSteps = D / 16;
+  // Two tiles (K and V, or Q and dO) at a time, in two sets where two workgroups then fit a compute unit: one is written while the other
+  // is read, and the workgroup meets once per tile.
+  static constexpr int kPair = 2 * kAttnTile * kPitch, kSets = 2 * kPair <= 72 * 1024 ? 2 : 1;
+  template <int ROWS, int THREADS> using Stage = AttnStage<_Float16, ROWS, kBytes, kPitch, THREADS>;
+};
 // The own operand: pieces of row `lane % 32`, the half of the lane.
-template <typename T, int D>
-__device__ __forceinline__ void attn_load_own(AttnOwn<T, D>& f, const T* row, bool valid, int d, int half) {
-  using Tile = AttnTile<T, D>;
+template <int D, int TERMS> struct AttnOwn {
+  f16x8 v[TERMS][D / 16];
+  // base: a row that is there, whether or not this lane's is
+  __device__ __forceinline__ void load(const _Float16* base, int64_t offset, bool valid, int d, int half) {
+    const _Float16* row = base + (valid ? offset : 0);
 #pragma unroll
-  for (int s = 0; s < Tile::kSteps; ++s) {
-    f[s] = typename AttnType<T>::Piece{};
-    if (valid) f[s] = attn_load_piece<T>(row, (2 * s + half) * Tile::kPiece, d);
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) v[t][s] = attn_load_whole_piece<_Float16>(row, t * D + (2 * s + half) * 8, d, valid);
   }
-}
+  __device__ __forceinline__ void negate() {
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) v[t][s] = -v[t][s];
+  }
+};
 
 // X += (32 rows of the tile) (own)^T
-template <int D>
-__device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const AttnOwn<_Float16, D>& own, int lane) {
-  using Tile = AttnTile<_Float16, D>;
-  const char* row = lds + (lane & 31) * Tile::kPitch + (lane >> 5) * 16;
+template <int D, int TERMS>
+__device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const AttnOwn<D, TERMS>& own, int lane) {
+  const char* row = lds + (lane & 31) * AttnTile<D, TERMS>::kPitch + (lane >> 5) * 16;
+  f16x8 a[TERMS][D / 16];
 #pragma unroll
-  for (int s = 0; s < Tile::kSteps; ++s)
-    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(row + s * 32), own[s], x, 0, 0, 0);
-}
-template <int D>
-__device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const AttnOwn<float, D>& own, int lane) {
-  using Tile = AttnTile<float, D>;
-  const char* row = lds + (lane & 31) * Tile::kPitch + (lane >> 5) * 16;
+  for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-  for (int s = 0; s < Tile::kSteps; ++s) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(row + s * 32);
+    for (int t = 0; t < TERMS; ++t) a[t][s] = *reinterpret_cast<const f16x8*>(row + t * D * 2 + s * 32);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], own[s][e], x, 0, 0, 0);
+  for (int s = 0; s < D / 16; ++s) {
+    if constexpr (TERMS == 2) {
+      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][s], own.v[0][s], x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][s], own.v[1][s], x, 0, 0, 0);
+    }
+    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][s], own.v[0][s], x, 0, 0, 0);
   }
+  // the reads run ahead of the products by four, rather than each product waiting for its own
+  constexpr int kReads = TERMS * D / 16, kAhead = kReads < 4 ? kReads : 4, kPer = TERMS == 2 ? 3 : 1;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = kAhead; i < kReads; i += TERMS) {
+    __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, TERMS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kPer * kAhead / TERMS, 0);
 }
 
 // acc (D x 32, blocks of 32) += (32 rows of the tile)^T X
-template <int D>
-__device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, _Float16) {
-  using Tile = AttnTile<_Float16, D>;
+template <int D, int TERMS>
+__device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane) {
   typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  constexpr int kPitch = AttnTile<D, TERMS>::kPitch;
   const int i = lane & 15;
-  const char* at = lds + (4 * (lane >> 5) + (i >> 2)) * Tile::kPitch + (((lane >> 4) & 1) * 16 + (i & 3) * 4) * 2;
+  const char* at = lds + (4 * (lane >> 5) + (i >> 2)) * kPitch + (((lane >> 4) & 1) * 16 + (i & 3) * 4) * 2;
+  auto left = [&](int s, int offset) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s) * kPitch + offset));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s + 8) * kPitch + offset));
+    return __builtin_bit_cast(f16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    f16x8 b;
+    f16x8 b, rest;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) b[e] = (_Float16)x[8 * s + e];         // to nearest: weights cut off would be too small in the mean
-#pragma unroll
-    for (int blk = 0; blk < D / 32; ++blk) {
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s) * Tile::kPitch + blk * 64));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s + 8) * Tile::kPitch + blk * 64));
-      typedef short s16x8 __attribute__((ext_vector_type(8)));
-      const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), b, acc[blk], 0, 0, 0);
+    for (int e = 0; e < 8; ++e) {
+      b[e] = (_Float16)x[8 * s + e];                     // to nearest: weights cut off would be too small in the mean
+      if constexpr (TERMS == 2) rest[e] = (_Float16)(x[8 * s + e] - (float)b[e]);
     }
-  }
-}
-template <int D>
-__device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, float) {
-  using Tile = AttnTile<float, D>;
-  const char* at = lds + 4 * (lane >> 5) * Tile::kPitch + (lane & 31) * 4;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
 #pragma unroll
     for (int blk = 0; blk < D / 32; ++blk) {
-      const float a = *reinterpret_cast<const float*>(at + (8 * (r / 4) + r % 4) * Tile::kPitch + blk * 128);
-      acc[blk] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, x[r], acc[blk], 0, 0, 0);
+      const f16x8 a = left(s, blk * 64);
+      if constexpr (TERMS == 2) {
+        acc[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left(s, D * 2 + blk * 64), b, acc[blk], 0, 0, 0);
+        acc[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, rest, acc[blk], 0, 0, 0);
+      }
+      acc[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc[blk], 0, 0, 0);
     }
   }
 }
 
-__device__ __forceinline__ float attn_other_half(float v) { return __shfl_xor(v, 32); }
+// Lanes l and l + 32 together, in both.
+__device__ __forceinline__ float attn_max_halves(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+__device__ __forceinline__ float attn_sum_halves(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
 
 // Stores D x 32 accumulators as rows of the output: lane l has row l % 32, four neighbouring elements at a time.
 template <typename T, int D>
@@ -264,20 +318,86 @@ __device__ __forceinline__ int attn_work(int id, int total) {
   return xcd * each + min(xcd, rest) + (id >> 3);
 }
 
+template <typename T> constexpr int attn_terms() { return sizeof(T) == 4 ? 2 : 1; }
+
+// How many of its states a sequence has.
+__device__ __forceinline__ int attn_seen(const AttnArgs& a, int batch) { return a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k; }
+
+// The panel of 128 queries that a workgroup works on, and which part of the keys.
+struct AttnPanelOf {
+  int split, panel, batch, kv_head, head, panels;
+  __device__ __forceinline__ AttnPanelOf(const AttnArgs& a, int rows) {
+    panels = (rows + kAttnPanel - 1) / kAttnPanel;
+    int work = attn_work(blockIdx.x, gridDim.x);
+    split = work % a.splits;
+    work /= a.splits;
+    panel = work % panels;
+    work /= panels;
+    const int of_group = work % a.group;
+    work /= a.group;
+    batch = work % a.batch;
+    kv_head = work / a.batch;
+    head = kv_head * a.group + of_group;
+  }
+};
+__device__ __forceinline__ void attn_tiles_of_split(const AttnArgs& a, int split, int seen, int& begin, int& end) {
+  const int all = (a.k + kAttnTile - 1) / kAttnTile;
+  begin = (int)((int64_t)all * split / a.splits);
+  end = min((int)((int64_t)all * (split + 1) / a.splits), (seen + kAttnTile - 1) / kAttnTile);
+}
+
+// The tiles in which a panel of 128 rows (two sets of 64) sees anything.
+struct AttnSeenTiles {
+  const uint64_t *a = nullptr, *b = nullptr;
+  __device__ __forceinline__ AttnSeenTiles(const uint64_t* mask, int64_t at, int64_t tiles, int64_t sets, int first_row) {
+    if (!mask) return;
+    const int64_t per = (tiles + 63) / 64;
+    a = mask + at + (first_row >> 6) * per;
+    if ((first_row >> 6) + 1 < sets) b = a + per;
+  }
+  __device__ __forceinline__ int next(int t, int end) const { return attn_next_tile(t, end, a, b); }
+};
+
+// Which of a tile's 64 positions a row sees, by the mask, and the first `left` of them.
+__device__ __forceinline__ uint64_t attn_word(const uint64_t* words, int row, bool valid) { return words ? valid ? words[row] : 0ull : ~0ull; }
+__device__ __forceinline__ uint64_t attn_first(uint64_t word, int left) {
+  return left >= 64 ? word : left > 0 ? word & ((1ull << left) - 1) : 0ull;
+}
+
+// What products of operands have to be multiplied by: 1 in half precision, whose operands are as they are.
+struct AttnFactors { float q, k, v, g; };
+template <typename T> __device__ __forceinline__ AttnFactors attn_factors(const AttnArgs& a, int batch, int kv_head) {
+  if constexpr (sizeof(T) == 2) return {1.f, 1.f, 1.f, 1.f};
+  const float* f = a.factors + ((int64_t)batch * a.kv_heads + kv_head) * 4;
+  return {f[0], f[1], f[2], f[3]};
+}
+
+// Scores of a block of 32 x 32: the scale and the bias.  from: the entry of the bias table for the lane's column and row 0 of the
+// block; a row further on is `STEP` entries further on.
+template <int STEP> __device__ __forceinline__ void attn_add_bias(f32x16& x, float scale, const float* from) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, from[STEP * (8 * (r / 4) + r % 4)]);
+}
+__device__ __forceinline__ void attn_add_constant(f32x16& x, float scale, float bias) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, bias);
+}
+
 // One row's running softmax: columns of 32 x 32 scores in 16 registers, two lanes to a column.
 struct AttnRunning { float most = -__builtin_inff(), sum = 0.f; };
 
 // x: NB blocks of scores, as the product left them (BIAS: scaled and biased already); turns them into weights relative to the
 // running maximum and scales what has been summed before.  c: what the exponent is multiplied by to be one of 2.
-template <typename T, int D, int NB, bool BIAS>
+template <int D, int NB, bool BIAS>
 __device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& run, f32x16 (&acc)[D / 32], float c) {
   float most = -__builtin_inff();
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) most = fmaxf(most, x[b][r]);
-  most = fmaxf(most, attn_other_half(most));
+  most = attn_max_halves(most);
   if (__any(most > run.most)) {
+    asm volatile("");
     const float now = fmaxf(run.most, most);
     // a column that has seen nothing yet has nothing to be scaled: its factor is 0, and (-inf) - (-inf) is not formed
     const float factor = run.most == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((run.most - now) * c);
@@ -288,13 +408,13 @@ __device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& 
   }
   const float base = run.most == -__builtin_inff() ? 0.f : run.most;
   // Scores of a bias are subtracted first: a bias of the type's lowest value times log2 e would be an infinity.
-  const float shift = BIAS ? base : AttnType<T>::kOffset - base * c;
+  const float shift = BIAS ? base : kOffset - base * c;
   float sum = 0.f;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      x[b][r] = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - shift, c, AttnType<T>::kOffset))
+      x[b][r] = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - shift, c, kOffset))
                      : __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, shift));
       sum += x[b][r];
     }
@@ -303,6 +423,7 @@ __device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& 
 
 // Scores that a column does not see become -inf.  word: bit per row of the block.
 __device__ __forceinline__ void attn_hide(f32x16& x, unsigned word, int half) {
+  asm volatile("");                                      // keeps the caller's branch: two instructions per score are not for every tile
   const unsigned w = word >> (4 * half);
 #pragma unroll
   for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? x[r] : -__builtin_inff();

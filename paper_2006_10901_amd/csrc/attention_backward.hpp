@@ -1,19 +1,20 @@
 // Gradients of attention.  With P = exp(s - lse), D_i = dO_i . O_i and dS_ij = P_ij (dO_i . V_j - D_i):
 //   dV_j = sum_i P_ij dO_i,   dK_j = scale sum_i dS_ij Q_i,   dQ_i = scale sum_j dS_ij K_j,   dtable[bucket] = sum of dS over its positions.
-// Two kernels form the scores again, one by panels of queries (dQ, the bias, and D, which it leaves for the other), one by panels of
-// keys (dK and dV): each sum has one owner, so that nothing is added up in an order that changes from call to call.
+// Two kernels form the scores again, one by panels of queries (dQ, and D, which it leaves for the others), one by panels of keys (dK
+// and dV): each sum has one owner, so that nothing is added up in an order that changes from call to call.  A third goes over the
+// positions near the diagonal for the gradient of the bias.
 #pragma once
 #include "attention.hpp"
 
 namespace spdl {
 
-// fp16 instructions take dS in half precision, whose range it may leave either way (it is as large as dO and as small as a weight
-// of a long row): it is taken times a power of two, the wave's own, lowered when a larger one comes along.  Numbers down to 2^-25 of
-// the largest so far then keep all their bits.
+// The instructions take dS in fp16 terms, whose range it may leave either way (it is as large as dO and as small as a weight of a long
+// row): it is taken times a power of two, the wave's own, lowered when a larger one comes along.  Numbers down to 2^-25 of the largest
+// so far then keep all bits of a term.
 struct AttnScale {
   float factor = 1.f, limit = 0.f;
-  // makes room for x; what has been summed is scaled along
-  template <int BLOCKS> __device__ __forceinline__ void fit(const f32x16& x, f32x16 (&acc)[BLOCKS]) {
+  // makes room for x and scales it; what has been summed is scaled along
+  template <int BLOCKS> __device__ __forceinline__ void fit(f32x16& x, f32x16 (&acc)[BLOCKS]) {
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[r]));
@@ -29,30 +30,177 @@ struct AttnScale {
       factor = now;
       limit = 32768.f / now;
     }
+    x *= factor;
   }
 };
 
-template <typename T, int BLOCKS> __device__ __forceinline__ void attn_fit(AttnScale& s, f32x16& x, f32x16 (&acc)[BLOCKS]) {
-  if constexpr (sizeof(T) == 2) {
-    s.fit(x, acc);
+// Whether all relative positions of a block of 32 x 32 lie at the clamped ends of a bias; near: that of its first key and first query.
+__device__ __forceinline__ bool attn_far(int near, int span) { return near - 31 >= span || near + 31 <= -span; }
+
+// What a row leaves for the gradient of the bias: the sum of all dS (0, but for the error of D), and those of dS and P over the
+// blocks that lie at the lower and at the upper end.
+// Added up in 64 bits: sums of thousands of terms that nearly cancel.
+struct AttnRowSums { double all, low, low_p, high, high_p; };
+
+// A workgroup's panel of queries for the backward pass.
+template <typename T, int D, bool BIAS> struct AttnQueries {
+  static constexpr int kTerms = attn_terms<T>();
+  AttnOwn<D, kTerms> q, g;
+  float scale, c, shift, to_dp;
+  int64_t flat;
+  __device__ __forceinline__ void load(const AttnArgs& a, const AttnPanelOf& at, const AttnFactors& f, int row, bool valid, int half) {
+    flat = ((int64_t)at.batch * a.heads + at.head) * a.m + row;
+    q.load(a.q16 + at.batch * a.q16s.batch + at.head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
+    g.load(a.g16 + at.batch * a.g16s.batch + at.head * a.g16s.head, row * a.g16s.row, valid, a.width, half);
+    if (a.scale < 0.f) q.negate();
+    scale = fabsf(a.scale) * (f.q * f.k);
+    c = BIAS ? kLog2e : scale * kLog2e;
+    to_dp = f.g * f.v;
+    float lse = valid ? a.lse[flat] : 0.f;
+    if (lse == -__builtin_inff()) lse = __builtin_inff();  // a row that sees nothing has no weights
+    shift = BIAS ? lse : -lse * kLog2e;
+  }
+  // x, y: Q K^T and dO V^T as the products leave them; x becomes P
+  __device__ __forceinline__ float weight(float x) const {
+    return BIAS ? __builtin_amdgcn_exp2f((x - shift) * c) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, shift));
+  }
+};
+
+// dQ, by panels of 128 queries, and D = dO . O.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
+  constexpr int kTerms = attn_terms<T>();
+  using Tile = AttnTile<D, kTerms>;
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
+
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
+  const AttnPanelOf at(a, a.m);
+  const int batch = at.batch, head = at.head, kv_head = at.kv_head;
+  const int seen = attn_seen(a, batch);
+  int begin, end;
+  attn_tiles_of_split(a, at.split, seen, begin, end);
+  const int first_row = at.panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
+  const bool valid = row < a.m;
+
+  const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
+  const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
+  const AttnFactors f = attn_factors<T>(a, batch, kv_head);
+  AttnQueries<T, D, BIAS> own;
+  own.load(a, at, f, row, valid, half);
+  float delta = 0.f;
+  if (valid) {
+    constexpr int kPiece = 16 / sizeof(T);
+    const T* O = static_cast<const T*>(a.O) + batch * a.o.batch + head * a.o.head + (int64_t)row * a.o.row;
+    const T* dO = static_cast<const T*>(a.dO) + batch * a.dout.batch + head * a.dout.head + (int64_t)row * a.dout.row;
+    if (a.d % kPiece == 0) {
+#pragma unroll 4
+      for (int c = half * kPiece; c < a.d; c += 2 * kPiece) {
+        const typename AttnPiece<T>::Type o = *reinterpret_cast<const typename AttnPiece<T>::Any*>(O + c),
+                                          g = *reinterpret_cast<const typename AttnPiece<T>::Any*>(dO + c);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] *= s.factor;
+        for (int e = 0; e < kPiece; ++e) delta = __builtin_fmaf((float)o[e], (float)g[e], delta);
+      }
+    } else {
+      for (int c = half; c < a.d; c += 2) delta = __builtin_fmaf((float)O[c], (float)dO[c], delta);
+    }
+  }
+  delta = attn_sum_halves(delta);
+  if (valid && half == 0 && at.split == 0) a.delta[own.flat] = delta;
+
+  const MaskLayout lay(a.m, a.k);
+  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
+  int position = 0;
+  if (BIAS) {
+    attn_fill_bias<T>(lds_bias, a, head, tid, 256);
+    position = attn_position(a, batch);
+  }
+  AttnRowSums sums = {};
+
+  f32x16 acc[D / 32] = {};
+  AttnScale ds_scale;
+  typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  uint64_t word_next = 0;
+  auto load = [&](int t) {
+    word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+  };
+  int t = tiles.next(begin, end);
+  if (t < end) load(t);
+  for (int set = 0; t < end; set ^= Tile::kSets - 1) {
+    char* lds_k = lds_raw + set * Tile::kPair;
+    char* lds_v = lds_k + kAttnTile * Tile::kPitch;
+    if (Tile::kSets == 1) __syncthreads();
+    stage_k.store(lds_k, tid);
+    stage_v.store(lds_v, tid);
+    const int key0 = t * kAttnTile;
+    const uint64_t word = attn_first(word_next, seen - key0);
+    __syncthreads();
+    t = tiles.next(t + 1, end);
+    if (t < end) load(t);
+    if (wave_row >= a.m || !__any(word != 0)) continue;
+    const bool hide = __any(word != ~0ull);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int near = key0 + 32 * b - (position + wave_row);   // relative position of the block's first key and first query
+      f32x16 x = {}, y = {};
+      attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+      attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+      const bool far = BIAS && attn_far(near, a.span);
+      if (BIAS) {
+        if (far) attn_add_constant(x, own.scale, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
+        else attn_add_bias<1>(x, own.scale, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+      }
+      const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
+      float sum = 0.f, sum_p = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float p = own.weight(x[r]);
+        if (hide) p = attn_bit(w, r) ? p : 0.f;
+        x[r] = p * __builtin_fmaf(y[r], own.to_dp, -delta);
+        if (hide) x[r] = attn_bit(w, r) ? x[r] : 0.f;      // whatever stands where the row does not look
+        if (BIAS) {
+          sum += x[r];
+          sum_p += p;
+        }
+      }
+      if (BIAS) {
+        sums.all += sum;
+        if (far) {
+          (near > 0 ? sums.high : sums.low) += sum;
+          (near > 0 ? sums.high_p : sums.low_p) += sum_p;
+        }
+      }
+      ds_scale.fit(x, acc);
+      attn_product_t<D, kTerms>(acc, lds_k + b * 32 * Tile::kPitch, x, lane);
+    }
+  }
+
+  const float factor = a.scale * f.k / ds_scale.factor;
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
+  if (a.splits == 1) {
+    T* dQ = static_cast<T*>(a.dQ) + batch * a.dq.batch + head * a.dq.head + (int64_t)row * a.dq.row;
+    attn_store_rows<T, D>(dQ, valid, acc, factor, a.d, half);
+  } else {
+    attn_store_rows<float, D>(a.part + (at.split * rows + own.flat) * a.d, valid, acc, factor, a.d, half);
+  }
+  if (BIAS && a.row_sums) {
+    double* to = a.row_sums + (at.split * rows + own.flat) * 5;
+    double s[5] = {sums.all, sums.low, sums.low_p, sums.high, sums.high_p};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      s[i] += __shfl_xor(s[i], 32);
+      if (valid && half == 0) to[i] = s[i];
+    }
   }
 }
 
 // Sums of dS by relative position, a wave's own: x holds keys in its registers and queries in its lanes.  The block of 32 x 32 goes
 // through LDS, and lane l sums the l-th diagonal.  Each relative position between the clamped ends then has one lane that adds it.
-__device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block, float* sums, int near, int span, float& low, float& high,
-                                                   int lane) {
+__device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block, float* sums, int near, int span, double& low,
+                                                   double& high, int lane) {
   const int half = lane >> 5;
-  if (near - 31 >= span || near + 31 <= -span) {          // all of it beyond an end
-    float s = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s += x[r];
-    if (near > 0) high += s;
-    else low += s;
-    return;
-  }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -61,9 +209,11 @@ __device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block
   __builtin_amdgcn_wave_barrier();
   const int off = lane - 31;                              // key minus query within the block
   float s = 0.f;
+#pragma unroll 8
   for (int i = 0; i < 32; ++i) {
     const int j = i + off;
-    if (j >= 0 && j < 32) s += block[i * 33 + j];
+    const float v = block[i * 33 + min(max(j, 0), 31)];
+    s += j >= 0 && j < 32 ? v : 0.f;
   }
   const int rel = near + off;
   if (lane < 63) {
@@ -73,182 +223,118 @@ __device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block
   }
 }
 
-constexpr int kAttnDiagBytes = 32 * 33 * 4;               // per wave
+constexpr int kAttnDiagonalBlock = 32 * 33;               // floats per wave
 
-// dQ, by panels of 128 queries, and D = dO . O.
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
-  using Tile = AttnTile<T, D>;
+// The gradient of the bias by relative position, by panels of 128 queries.  In half precision D is off by what rounding O cost, by as
+// much as a bucket's sum of dS, whose terms nearly cancel, is off; but over a row dS adds up to 0, so that the sum that it gave with that
+// D is D's error, and dS less that times P is right.  Where relative positions lie at the ends of the bias, the sums that
+// attention_dq_kernel left of each row are put right so; the blocks near the diagonal are formed again with the right D.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) {
+  constexpr int kTerms = attn_terms<T>();
+  using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  char* lds_k = lds_raw;
-  char* lds_v = lds_raw + kAttnTile * Tile::kPitch;
-  float* lds_bias = reinterpret_cast<float*>(lds_raw + 2 * kAttnTile * Tile::kPitch);
+  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
+  float* lds_blocks = lds_bias + attn_bias_entries(a.span);
+  float* lds_sums = lds_blocks + kAttnWaves * kAttnDiagonalBlock;
+  const int n = 2 * a.span + 1;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
-  const int panels = (a.m + kAttnPanel - 1) / kAttnPanel;
-  int work = attn_work(blockIdx.x, gridDim.x);
-  const int split = work % a.splits;
-  work /= a.splits;
-  const int panel = work % panels;
-  work /= panels;
-  const int of_group = work % a.group;
-  work /= a.group;
-  const int batch = work % a.batch, kv_head = work / a.batch, head = kv_head * a.group + of_group;
-
-  const int seen = a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k;
-  const int tiles_all = (a.k + kAttnTile - 1) / kAttnTile;
-  const int begin = (int)((int64_t)tiles_all * split / a.splits);
-  const int end = min((int)((int64_t)tiles_all * (split + 1) / a.splits), (seen + kAttnTile - 1) / kAttnTile);
-  const int first_row = panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
+  const AttnPanelOf at(a, a.m);                           // a.splits is 1 here, row_splits those that left row_sums
+  const int batch = at.batch, head = at.head, kv_head = at.kv_head;
+  const int seen = attn_seen(a, batch);
+  const int first_row = at.panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
   const bool valid = row < a.m;
-  const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
+  const int position = attn_position(a, batch);
+  // tiles that hold relative positions between the ends
+  const int lowest = position + first_row - a.span - kAttnTile, highest = position + first_row + kAttnPanel + a.span;
+  const int begin = max(lowest, 0) / kAttnTile, end = min((seen + kAttnTile - 1) / kAttnTile, max(highest, 0) / kAttnTile + 1);
 
-  const T* Q = static_cast<const T*>(a.Q) + batch * a.q.batch + head * a.q.head;
-  const T* K = static_cast<const T*>(a.K) + batch * a.kk.batch + kv_head * a.kk.head;
-  const T* V = static_cast<const T*>(a.V) + batch * a.v.batch + kv_head * a.v.head;
-  const T* O = static_cast<const T*>(a.O) + batch * a.o.batch + head * a.o.head;
-  const T* dO = static_cast<const T*>(a.dO) + batch * a.dout.batch + head * a.dout.head;
+  const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
+  const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
+  const AttnFactors f = attn_factors<T>(a, batch, kv_head);
+  AttnQueries<T, D, true> own;
+  own.load(a, at, f, row, valid, half);
+  attn_fill_bias<T>(lds_bias, a, head, tid, 256);
+  float* sums = lds_sums + wave * n;
+  for (int x = lane; x < n; x += 64) sums[x] = 0.f;
 
-  AttnOwn<T, D> q, g;
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   float delta = 0.f;
-  {
-    AttnOwn<T, D> o;
-    attn_load_own<T, D>(o, O + (int64_t)row * a.o.row, valid, a.d, half);
-    attn_load_own<T, D>(g, dO + (int64_t)row * a.dout.row, valid, a.d, half);
-#pragma unroll
-    for (int s = 0; s < Tile::kSteps; ++s)
-#pragma unroll
-      for (int e = 0; e < Tile::kPiece; ++e) delta = __builtin_fmaf((float)o[s][e], (float)g[s][e], delta);
-    delta += attn_other_half(delta);
+  double low = 0., high = 0.;
+  if (valid) {
+    AttnRowSums s = {};
+    for (int i = 0; i < a.row_splits; ++i) {
+      const double* from = a.row_sums + (i * rows + own.flat) * 5;
+      s.all += from[0], s.low += from[1], s.low_p += from[2], s.high += from[3], s.high_p += from[4];
+    }
+    delta = (float)(a.delta[own.flat] + s.all);
+    if (half == 0) low = s.low - s.all * s.low_p, high = s.high - s.all * s.high_p;
   }
-  if (valid && half == 0 && split == 0) a.delta[flat] = delta;
-  attn_load_own<T, D>(q, Q + (int64_t)row * a.q.row, valid, a.d, half);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int s = 0; s < Tile::kSteps; ++s) q[s] = -q[s];
-  }
-  const float scale = fabsf(a.scale);
-  const float c = BIAS ? kLog2e : scale * kLog2e;
-  float lse = valid ? a.lse[flat] : 0.f;
-  if (lse == -__builtin_inff()) lse = __builtin_inff();   // a row that sees nothing has no weights
-  const float shift = BIAS ? lse : -lse * kLog2e;
 
   const MaskLayout lay(a.m, a.k);
-  const uint64_t *tiles_a = nullptr, *tiles_b = nullptr;
-  if (a.mask) {
-    const int64_t per = (lay.tj + 63) / 64;
-    tiles_a = a.mask + lay.row_tiles + (int64_t)(first_row >> 6) * per;
-    if ((first_row >> 6) + 1 < lay.ti) tiles_b = tiles_a + per;
-  }
-  int position = 0;
-  float *diag_block = nullptr, *diag_sums = nullptr, low = 0.f, high = 0.f;
-  if (BIAS) {
-    attn_fill_bias<T>(lds_bias, a, head, tid, 256);
-    position = attn_position(a, batch);
-    if (a.part_bias) {
-      float* after = lds_bias + attn_bias_entries(a.span);
-      diag_block = after + wave * (32 * 33);
-      diag_sums = after + kAttnWaves * (32 * 33) + wave * (2 * a.span + 1);
-      for (int x = lane; x < 2 * a.span + 1; x += 64) diag_sums[x] = 0.f;
-    }
-  }
-
-  f32x16 acc[D / 32] = {};
-  AttnScale ds_scale;
-  AttnStage<T, D, kAttnTile, 256> stage_k, stage_v;
-  int t = attn_next_tile(begin, end, tiles_a, tiles_b);
-  if (t < end) {
-    stage_k.load(K + (int64_t)t * kAttnTile * a.kk.row, a.kk.row, seen - t * kAttnTile, a.d, tid);
-    stage_v.load(V + (int64_t)t * kAttnTile * a.v.row, a.v.row, seen - t * kAttnTile, a.d, tid);
-  }
-  while (t < end) {
-    __syncthreads();
+  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
+  typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  uint64_t word_next = 0;
+  auto load = [&](int t) {
+    word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+  };
+  int t = tiles.next(begin, end);
+  if (t < end) load(t);
+  for (int set = 0; t < end; set ^= Tile::kSets - 1) {
+    char* lds_k = lds_raw + set * Tile::kPair;
+    char* lds_v = lds_k + kAttnTile * Tile::kPitch;
+    if (Tile::kSets == 1) __syncthreads();
     stage_k.store(lds_k, tid);
     stage_v.store(lds_v, tid);
+    const int key0 = t * kAttnTile;
+    const uint64_t word = attn_first(word_next, seen - key0);
     __syncthreads();
-    const int here = t;
-    t = attn_next_tile(t + 1, end, tiles_a, tiles_b);
-    if (t < end) {
-      stage_k.load(K + (int64_t)t * kAttnTile * a.kk.row, a.kk.row, seen - t * kAttnTile, a.d, tid);
-      stage_v.load(V + (int64_t)t * kAttnTile * a.v.row, a.v.row, seen - t * kAttnTile, a.d, tid);
-    }
-    const int key0 = here * kAttnTile;
-    uint64_t word = ~0ull;
-    if (a.mask) word = valid ? a.mask[lay.row_words + (int64_t)here * lay.ti * 64 + row] : 0ull;
-    if (seen - key0 < 64) word &= (1ull << (seen - key0)) - 1;
+    t = tiles.next(t + 1, end);
+    if (t < end) load(t);
     if (wave_row >= a.m || !__any(word != 0)) continue;
-    const bool hide = __any(word != ~0ull);
-    const int near = key0 - (position + wave_row);
-#pragma unroll
     for (int b = 0; b < 2; ++b) {
+      const int near = key0 + 32 * b - (position + wave_row);
+      if (attn_far(near, a.span)) continue;
       f32x16 x = {}, y = {};
-      attn_product<D>(x, lds_k + b * 32 * Tile::kPitch, q, lane);
-      attn_product<D>(y, lds_v + b * 32 * Tile::kPitch, g, lane);
-      if (BIAS) {
-        if (near - 31 >= a.span || near + 63 <= -a.span) {
-          const float far = lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, far);
-        } else {
-          const float* at = lds_bias + kAttnPad + a.span + near + 32 * b - (lane & 31) + 4 * half;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, at[8 * (r / 4) + r % 4]);
-        }
-      }
+      attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+      attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+      attn_add_bias<1>(x, own.scale, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = BIAS ? __builtin_amdgcn_exp2f((x[r] - shift) * c) : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shift));
-        x[r] = p * (y[r] - delta);
-        if (hide) x[r] = attn_bit(w, r) ? x[r] : 0.f;
-      }
-      if (BIAS && a.part_bias) attn_sum_diagonals(x, diag_block, diag_sums, near + 32 * b, a.span, low, high, lane);
-      attn_fit<T>(ds_scale, x, acc);
-      attn_product_t<D>(acc, lds_k + b * 32 * Tile::kPitch, x, lane, T{});
+      for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? own.weight(x[r]) * __builtin_fmaf(y[r], own.to_dp, -delta) : 0.f;
+      attn_sum_diagonals(x, lds_blocks + wave * kAttnDiagonalBlock, sums, near, a.span, low, high, lane);
     }
   }
-
-  const float factor = a.scale / ds_scale.factor;
-  if (a.splits == 1) {
-    T* dQ = static_cast<T*>(a.dQ) + batch * a.dq.batch + head * a.dq.head + (int64_t)row * a.dq.row;
-    attn_store_rows<T, D>(dQ, valid, acc, factor, a.d, half);
-  } else {
-    const int64_t rows = (int64_t)a.batch * a.heads * a.m;
-    attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, valid, acc, factor, a.d, half);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    low += __shfl_xor(low, o);
+    high += __shfl_xor(high, o);
   }
-  if (BIAS && a.part_bias) {
+  if (lane == 0) {
+    sums[0] += (float)low;
+    sums[2 * a.span] += (float)high;
+  }
+  __syncthreads();
+  float* to = a.part_bias + (((int64_t)head * a.batch + batch) * at.panels + at.panel) * n;
+  for (int x = tid; x < n; x += 256) {
+    float s = 0.f;
 #pragma unroll
-    for (int o = 32; o; o >>= 1) {
-      low += __shfl_xor(low, o);
-      high += __shfl_xor(high, o);
-    }
-    if (lane == 0) {
-      diag_sums[0] += low;
-      diag_sums[2 * a.span] += high;
-    }
-    __syncthreads();
-    const int n = 2 * a.span + 1;
-    const float* from = lds_bias + attn_bias_entries(a.span) + kAttnWaves * (32 * 33);
-    float* to = a.part_bias + (((int64_t)head * a.batch + batch) * panels * a.splits + panel * a.splits + split) * n;
-    for (int x = tid; x < n; x += 256) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) s += from[w * n + x];
-      to[x] = s;
-    }
+    for (int w = 0; w < kAttnWaves; ++w) s += lds_sums[w * n + x];
+    to[x] = s;
   }
 }
 
 // dK and dV, by panels of 128 keys: a wave has 32 of them, tiles of 64 queries, of every head that shares the keys, are shared by the waves.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
-  using Tile = AttnTile<T, D>;
+  constexpr int kTerms = attn_terms<T>();
+  using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  char* lds_q = lds_raw;
-  char* lds_g = lds_raw + kAttnTile * Tile::kPitch;
-  float* lds_lse = reinterpret_cast<float*>(lds_raw + 2 * kAttnTile * Tile::kPitch);
-  float* lds_delta = lds_lse + kAttnTile;
-  float* lds_bias = lds_delta + kAttnTile;
+  float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set: 64 times lse, 64 times D
+  float* lds_bias = lds_stats + Tile::kSets * 2 * kAttnTile;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
   const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
@@ -259,7 +345,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   work /= panels;
   const int batch = work % a.batch, kv_head = work / a.batch;
 
-  const int seen = a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k;
+  const int seen = attn_seen(a, batch);
   const int first_key = panel * kAttnPanel, wave_key = first_key + wave * 32, key = wave_key + (lane & 31);
   const bool valid = key < seen;
   const int tiles = (a.m + kAttnTile - 1) / kAttnTile;
@@ -267,29 +353,20 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   const int64_t all = (int64_t)a.group * tiles;
   const int64_t begin = first_key < seen ? all * split / a.splits : 0, end = first_key < seen ? all * (split + 1) / a.splits : 0;
 
-  const T* K = static_cast<const T*>(a.K) + batch * a.kk.batch + kv_head * a.kk.head;
-  const T* V = static_cast<const T*>(a.V) + batch * a.v.batch + kv_head * a.v.head;
-  const T* Q = static_cast<const T*>(a.Q) + batch * a.q.batch + (int64_t)kv_head * a.group * a.q.head;
-  const T* dO = static_cast<const T*>(a.dO) + batch * a.dout.batch + (int64_t)kv_head * a.group * a.dout.head;
+  const _Float16* Q = a.q16 + batch * a.q16s.batch + (int64_t)kv_head * a.group * a.q16s.head;
+  const _Float16* dO = a.g16 + batch * a.g16s.batch + (int64_t)kv_head * a.group * a.g16s.head;
   const int64_t stat0 = ((int64_t)batch * a.heads + (int64_t)kv_head * a.group) * a.m;
 
-  AttnOwn<T, D> kf, vf;
-  attn_load_own<T, D>(kf, K + (int64_t)key * a.kk.row, valid, a.d, half);
-  attn_load_own<T, D>(vf, V + (int64_t)key * a.v.row, valid, a.d, half);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int s = 0; s < Tile::kSteps; ++s) kf[s] = -kf[s];
-  }
-  const float scale = fabsf(a.scale);
+  AttnOwn<D, kTerms> kf, vf;
+  kf.load(a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head, key * a.k16s.row, valid, a.width, half);
+  vf.load(a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head, key * a.v16s.row, valid, a.width, half);
+  if (a.scale < 0.f) kf.negate();
+  const AttnFactors f = attn_factors<T>(a, batch, kv_head);
+  const float scale = fabsf(a.scale) * (f.q * f.k), to_dp = f.g * f.v;
   const float c = BIAS ? kLog2e : scale * kLog2e;
 
   const MaskLayout lay(a.m, a.k);
-  const uint64_t *tiles_a = nullptr, *tiles_b = nullptr;
-  if (a.mask) {
-    const int64_t per = (lay.ti + 63) / 64;
-    tiles_a = a.mask + lay.col_tiles + (int64_t)(first_key >> 6) * per;
-    if ((first_key >> 6) + 1 < lay.tj) tiles_b = tiles_a + per;
-  }
+  const AttnSeenTiles seen_tiles(a.mask, lay.col_tiles, lay.ti, lay.tj, first_key);
   const int position = BIAS ? attn_position(a, batch) : 0;
 
   // the next (head of the group, tile of queries) that the panel takes part in
@@ -297,7 +374,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
     while (at < end) {
       const int h = (int)(at / tiles), t = (int)(at - (int64_t)h * tiles);
       const int stop = (int)min((int64_t)tiles, end - (int64_t)h * tiles);
-      const int n = attn_next_tile(t, stop, tiles_a, tiles_b);
+      const int n = seen_tiles.next(t, stop);
       if (n < stop) return (int64_t)h * tiles + n;
       at = (int64_t)h * tiles + stop;
     }
@@ -306,57 +383,56 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
 
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
   AttnScale ds_scale;
-  AttnStage<T, D, kAttnTile, 256> stage_q, stage_g;
+  typename Tile::template Stage<kAttnTile, 256> stage_q, stage_g;
   float stat = 0.f;
+  uint64_t word_next = 0;
   auto load = [&](int64_t at) {
     const int h = (int)(at / tiles), t = (int)(at - (int64_t)h * tiles), rows = a.m - t * kAttnTile;
-    stage_q.load(Q + h * a.q.head + (int64_t)t * kAttnTile * a.q.row, a.q.row, rows, a.d, tid);
-    stage_g.load(dO + h * a.dout.head + (int64_t)t * kAttnTile * a.dout.row, a.dout.row, rows, a.d, tid);
+    word_next = attn_word(a.mask ? a.mask + lay.col_words + (int64_t)t * lay.tj * 64 : nullptr, key, valid);
+    stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, tid);
+    stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, tid);
     const int r = tid & 63;
     if (tid < 128) stat = r < rows ? (tid < 64 ? a.lse : a.delta)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
   };
   int64_t at = next(begin);
   int bias_head = -1;
   if (at < end) load(at);
-  while (at < end) {
-    __syncthreads();
+  for (int set = 0; at < end; set ^= Tile::kSets - 1) {
+    char* lds_q = lds_raw + set * Tile::kPair;
+    char* lds_g = lds_q + kAttnTile * Tile::kPitch;
+    float* lds_lse = lds_stats + set * 2 * kAttnTile;
+    float* lds_delta = lds_lse + kAttnTile;
+    if (Tile::kSets == 1) __syncthreads();
     stage_q.store(lds_q, tid);
     stage_g.store(lds_g, tid);
     const int h = (int)(at / tiles), row0 = (int)(at - (int64_t)h * tiles) * kAttnTile;
     if (tid < 64) {
       // rows that see nothing, and those behind the last, have no weights
       const float l = stat == -__builtin_inff() ? __builtin_inff() : stat;
-      lds_lse[tid] = BIAS ? l : AttnType<T>::kOffset - l * kLog2e;
+      lds_lse[tid] = BIAS ? l : kOffset - l * kLog2e;
     } else if (tid < 128) {
       lds_delta[tid - 64] = stat;
     }
+    const uint64_t word = valid ? word_next : 0ull;
     if (BIAS && h != bias_head) {
+      if (Tile::kSets == 2) __syncthreads();              // the head before may still be at work
       attn_fill_bias<T>(lds_bias, a, kv_head * a.group + h, tid, 256);
       bias_head = h;
     }
     __syncthreads();
     at = next(at + 1);
     if (at < end) load(at);
-    uint64_t word = valid ? ~0ull : 0ull;
-    if (a.mask && valid) word = a.mask[lay.col_words + (int64_t)(row0 >> 6) * lay.tj * 64 + key];
     if (!__any(word != 0)) continue;
     const bool hide = __any(word != ~0ull);
-    const int near = wave_key - (position + row0);        // relative position of the wave's first key and the tile's first query
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      const int near = wave_key - (position + row0 + 32 * b);
       f32x16 x = {}, y = {};
-      attn_product<D>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
-      attn_product<D>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
+      attn_product<D, kTerms>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
+      attn_product<D, kTerms>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
       if (BIAS) {
-        if (near - 63 >= a.span || near + 31 <= -a.span) {
-          const float far = lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, far);
-        } else {
-          const float* from = lds_bias + kAttnPad + a.span + near - 32 * b + (lane & 31) - 4 * half;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, from[-(8 * (r / 4) + r % 4)]);
-        }
+        if (attn_far(near, a.span)) attn_add_constant(x, scale, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
+        else attn_add_bias<-1>(x, scale, lds_bias + kAttnPad + a.span + near + (lane & 31) - 4 * half);
       }
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
@@ -366,9 +442,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * q4 + e;
-          float p = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[r] - l[e], c, AttnType<T>::kOffset))
-                         : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, l[e]));
-          float s = p * (y[r] - dl[e]);
+          float p = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[r] - l[e], c, kOffset)) : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, l[e]));
+          float s = p * __builtin_fmaf(y[r], to_dp, -dl[e]);
           if (hide) {
             p = attn_bit(w, r) ? p : 0.f;
             s = attn_bit(w, r) ? s : 0.f;
@@ -377,59 +452,81 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
           y[r] = s;
         }
       }
-      attn_product_t<D>(dv, lds_g + b * 32 * Tile::kPitch, x, lane, T{});
-      attn_fit<T>(ds_scale, y, dk);
-      attn_product_t<D>(dk, lds_q + b * 32 * Tile::kPitch, y, lane, T{});
+      attn_product_t<D, kTerms>(dv, lds_g + b * 32 * Tile::kPitch, x, lane);
+      ds_scale.fit(y, dk);
+      attn_product_t<D, kTerms>(dk, lds_q + b * 32 * Tile::kPitch, y, lane);
     }
   }
 
-  const float offset = __builtin_amdgcn_exp2f(-AttnType<T>::kOffset);
+  const float offset = __builtin_amdgcn_exp2f(-kOffset);
+  const float to_dk = a.scale * f.q * offset / ds_scale.factor, to_dv = f.g * offset;
   const bool stored = key < a.k;
   if (a.splits == 1) {
     T* dK = static_cast<T*>(a.dK) + batch * a.dk.batch + kv_head * a.dk.head + (int64_t)key * a.dk.row;
     T* dV = static_cast<T*>(a.dV) + batch * a.dv.batch + kv_head * a.dv.head + (int64_t)key * a.dv.row;
-    attn_store_rows<T, D>(dK, stored, dk, a.scale / ds_scale.factor * offset, a.d, half);
-    attn_store_rows<T, D>(dV, stored, dv, offset, a.d, half);
+    attn_store_rows<T, D>(dK, stored, dk, to_dk, a.d, half);
+    attn_store_rows<T, D>(dV, stored, dv, to_dv, a.d, half);
   } else {
     const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k, flat = ((int64_t)batch * a.kv_heads + kv_head) * a.k + key;
-    attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, stored, dk, a.scale / ds_scale.factor * offset, a.d, half);
-    attn_store_rows<float, D>(a.part + ((a.splits + split) * rows + flat) * a.d, stored, dv, offset, a.d, half);
+    attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, stored, dk, to_dk, a.d, half);
+    attn_store_rows<float, D>(a.part + ((a.splits + split) * rows + flat) * a.d, stored, dv, to_dv, a.d, half);
   }
 }
 
-// Adds up what `splits` workgroups left of each of the rows, in their order.
+// Adds up what `splits` workgroups left of each of the rows, in their order: of one array, or of two that lie one behind the other.
+struct AttnSum { AttnStrides to; void* out; };
 template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part,
-                                                            AttnStrides to, T* out) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= rows * d) return;
+__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part, AttnSum first,
+                                                            AttnSum second) {
+  int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool behind = at >= rows * d;
+  if (behind) {
+    at -= rows * d;
+    part += splits * rows * d;
+  }
+  const AttnSum& x = behind ? second : first;
+  if (at >= rows * d || !x.out) return;
   const int64_t flat = at / d;
   const int col = (int)(at - flat * d);
   float s = 0.f;
   for (int i = 0; i < splits; ++i) s += part[(int64_t)i * rows * d + at];
   const int64_t bh = flat / per_head;
-  out[bh / heads * to.batch + bh % heads * to.head + (flat % per_head) * to.row + col] = (T)s;
+  static_cast<T*>(x.out)[bh / heads * x.to.batch + bh % heads * x.to.head + (flat % per_head) * x.to.row + col] = (T)s;
 }
 
-// dtable of one head: the workgroups' sums by relative position, in their order, then those of a bucket, in ascending position.
+// dtable of one head: the panels' sums by relative position (sixteen waves take panels in turn, then are added up in their order), then
+// those of a bucket, in ascending position.
 template <typename T>
 __global__ __launch_bounds__(1024) void attention_dtable_kernel(const AttnArgs a, int parts, T* dtable) {
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  float* sums = reinterpret_cast<float*>(lds_raw);
-  const int n = 2 * a.span + 1, head = blockIdx.x;
+  double* sums = reinterpret_cast<double*>(lds_raw);
+  int* buckets = reinterpret_cast<int*>(sums + 2 * a.span + 1);
+  __shared__ double waves[16][64];
+  const int n = 2 * a.span + 1, head = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float* from = a.part_bias + (int64_t)head * parts * n;
-  for (int x = threadIdx.x; x < n; x += 1024) {
-    float s = 0.f;
-    for (int i = 0; i < parts; ++i) s += from[(int64_t)i * n + x];
-    sums[x] = s;
+  for (int x0 = 0; x0 < n; x0 += 64) {
+    const int x = min(x0 + lane, n - 1);
+    double s = 0.;
+#pragma unroll 4
+    for (int i = wave; i < parts; i += 16) s += from[(int64_t)i * n + x];
+    waves[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && x0 + lane < n) {
+      double all = 0.;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) all += waves[w][lane];
+      sums[x] = all;
+      buckets[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int b = threadIdx.x; b < a.buckets; b += 1024) {
-    float s = 0.f;
-    for (int x = 0; x < n; ++x)
-      if (min(max(a.bucket_of[x], 0), a.buckets - 1) == b) s += sums[x];
-    dtable[(int64_t)head * a.buckets + b] = (T)s;
-  }
+  // eight threads to a bucket, each an eighth of the positions
+  const int b = threadIdx.x >> 3, eighth = threadIdx.x & 7;
+  double s = 0.;
+  for (int x = n * eighth / 8; x < n * (eighth + 1) / 8; ++x) s += buckets[x] == b ? sums[x] : 0.;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
+  if (eighth == 0 && b < a.buckets) dtable[(int64_t)head * a.buckets + b] = (T)s;
 }
 
 }  // namespace spdl

@@ -5,63 +5,34 @@
 
 namespace spdl {
 
-// Scores of a block of 32 keys: the scale and the bias.  at: the entry of the bias table for row 0 of the block and the lane's query.
-__device__ __forceinline__ void attn_add_bias(f32x16& x, float scale, const float* at) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, at[8 * (r / 4) + r % 4]);
-}
-__device__ __forceinline__ void attn_add_constant(f32x16& x, float scale, float bias) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(x[r], scale, bias);
-}
-
 // Panels of 128 queries: a wave has 32 of them, tiles of 64 keys are shared by the four waves.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a) {
-  using Tile = AttnTile<T, D>;
+  constexpr int kTerms = attn_terms<T>();
+  using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  char* lds_k = lds_raw;
-  char* lds_v = lds_raw + kAttnTile * Tile::kPitch;
-  float* lds_bias = reinterpret_cast<float*>(lds_raw + 2 * kAttnTile * Tile::kPitch);
+  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
-  const int panels = (a.m + kAttnPanel - 1) / kAttnPanel;
-  int work = attn_work(blockIdx.x, gridDim.x);
-  const int split = work % a.splits;
-  work /= a.splits;
-  const int panel = work % panels;
-  work /= panels;
-  const int of_group = work % a.group;
-  work /= a.group;
-  const int batch = work % a.batch, kv_head = work / a.batch, head = kv_head * a.group + of_group;
-
-  const int seen = a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k;
-  const int tiles_all = (a.k + kAttnTile - 1) / kAttnTile;
-  const int begin = (int)((int64_t)tiles_all * split / a.splits);
-  const int end = min((int)((int64_t)tiles_all * (split + 1) / a.splits), (seen + kAttnTile - 1) / kAttnTile);
-  const int first_row = panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
+  const AttnPanelOf at(a, a.m);
+  const int batch = at.batch, head = at.head, kv_head = at.kv_head;
+  const int seen = attn_seen(a, batch);
+  int begin, end;
+  attn_tiles_of_split(a, at.split, seen, begin, end);
+  const int first_row = at.panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
   const bool valid = row < a.m;
 
-  const T* Q = static_cast<const T*>(a.Q) + batch * a.q.batch + head * a.q.head;
-  const T* K = static_cast<const T*>(a.K) + batch * a.kk.batch + kv_head * a.kk.head;
-  const T* V = static_cast<const T*>(a.V) + batch * a.v.batch + kv_head * a.v.head;
-
-  AttnOwn<T, D> q;
-  attn_load_own<T, D>(q, Q + (int64_t)row * a.q.row, valid, a.d, half);
-  if (a.scale < 0.f) {                                   // so that the largest score is the largest product
-#pragma unroll
-    for (int s = 0; s < Tile::kSteps; ++s) q[s] = -q[s];
-  }
-  const float scale = fabsf(a.scale);
+  const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
+  const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
+  AttnOwn<D, kTerms> q;
+  q.load(a.q16 + batch * a.q16s.batch + head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
+  if (a.scale < 0.f) q.negate();                         // so that the largest score is the largest product
+  const AttnFactors f = attn_factors<T>(a, batch, kv_head);
+  const float scale = fabsf(a.scale) * (f.q * f.k);
   const float c = BIAS ? kLog2e : fmaxf(scale * kLog2e, 1e-37f);   // never 0: it meets the -inf of hidden positions
 
   const MaskLayout lay(a.m, a.k);
-  const uint64_t *tiles_a = nullptr, *tiles_b = nullptr;
-  if (a.mask) {
-    const int64_t per = (lay.tj + 63) / 64;
-    tiles_a = a.mask + lay.row_tiles + (int64_t)(first_row >> 6) * per;
-    if ((first_row >> 6) + 1 < lay.ti) tiles_b = tiles_a + per;
-  }
+  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   int position = 0;
   if (BIAS) {
     attn_fill_bias<T>(lds_bias, a, head, tid, 256);
@@ -70,31 +41,30 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
 
   f32x16 acc[D / 32] = {};
   AttnRunning run;
-  AttnStage<T, D, kAttnTile, 256> stage_k, stage_v;
-  int t = attn_next_tile(begin, end, tiles_a, tiles_b);
-  if (t < end) {
-    stage_k.load(K + (int64_t)t * kAttnTile * a.kk.row, a.kk.row, seen - t * kAttnTile, a.d, tid);
-    stage_v.load(V + (int64_t)t * kAttnTile * a.v.row, a.v.row, seen - t * kAttnTile, a.d, tid);
-  }
-  while (t < end) {
-    __syncthreads();
+  typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  uint64_t word_next = 0;
+  auto load = [&](int t) {
+    word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+  };
+  int t = tiles.next(begin, end);
+  if (t < end) load(t);
+  for (int set = 0; t < end; set ^= Tile::kSets - 1) {
+    char* lds_k = lds_raw + set * Tile::kPair;
+    char* lds_v = lds_k + kAttnTile * Tile::kPitch;
+    if (Tile::kSets == 1) __syncthreads();
     stage_k.store(lds_k, tid);
     stage_v.store(lds_v, tid);
+    const int key0 = t * kAttnTile;
+    const uint64_t word = attn_first(word_next, seen - key0);
     __syncthreads();
-    const int here = t;
-    t = attn_next_tile(t + 1, end, tiles_a, tiles_b);
-    if (t < end) {
-      stage_k.load(K + (int64_t)t * kAttnTile * a.kk.row, a.kk.row, seen - t * kAttnTile, a.d, tid);
-      stage_v.load(V + (int64_t)t * kAttnTile * a.v.row, a.v.row, seen - t * kAttnTile, a.d, tid);
-    }
-    const int key0 = here * kAttnTile;
-    uint64_t word = ~0ull;
-    if (a.mask) word = valid ? a.mask[lay.row_words + (int64_t)here * lay.ti * 64 + row] : 0ull;
-    if (seen - key0 < 64) word &= (1ull << (seen - key0)) - 1;
+    t = tiles.next(t + 1, end);
+    if (t < end) load(t);
     if (wave_row >= a.m || !__any(word != 0)) continue;   // none of the wave's queries sees the tile
     f32x16 x[2] = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) attn_product<D>(x[b], lds_k + b * 32 * Tile::kPitch, q, lane);
+    for (int b = 0; b < 2; ++b) attn_product<D, kTerms>(x[b], lds_k + b * 32 * Tile::kPitch, q, lane);
     if (BIAS) {
       const int near = key0 - (position + wave_row);     // relative position of the tile's first key and the wave's first query
       if (near - 31 >= a.span || near + 63 <= -a.span) {
@@ -102,24 +72,24 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
 #pragma unroll
         for (int b = 0; b < 2; ++b) attn_add_constant(x[b], scale, far);
       } else {
-        const float* at = lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half;
+        const float* from = lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) attn_add_bias(x[b], scale, at + 32 * b);
+        for (int b = 0; b < 2; ++b) attn_add_bias<1>(x[b], scale, from + 32 * b);
       }
     }
     if (__any(word != ~0ull)) {
       attn_hide(x[0], (unsigned)word, half);
       attn_hide(x[1], (unsigned)(word >> 32), half);
     }
-    attn_softmax_step<T, D, 2, BIAS>(x, run, acc, c);
+    attn_softmax_step<D, 2, BIAS>(x, run, acc, c);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) attn_product_t<D>(acc, lds_v + b * 32 * Tile::kPitch, x[b], lane, T{});
+    for (int b = 0; b < 2; ++b) attn_product_t<D, kTerms>(acc, lds_v + b * 32 * Tile::kPitch, x[b], lane);
   }
 
-  const float total = run.sum + attn_other_half(run.sum);
+  const float total = attn_sum_halves(run.sum);
   const bool none = run.most == -__builtin_inff() && total == 0.f;
-  const float lse = none ? -__builtin_inff() : run.most * c * kLn2 + (__builtin_amdgcn_logf(total) - AttnType<T>::kOffset) * kLn2;
-  const float inv = none ? 0.f : 1.f / total;
+  const float lse = none ? -__builtin_inff() : run.most * c * kLn2 + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
+  const float inv = none ? 0.f : f.v / total;
   const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
   if (a.splits == 1) {
     T* O = static_cast<T*>(a.O) + batch * a.o.batch + head * a.o.head + (int64_t)row * a.o.row;
@@ -127,8 +97,48 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
     if (valid && half == 0 && a.lse) a.lse[flat] = lse;
   } else {
     const int64_t rows = (int64_t)a.batch * a.heads * a.m;
-    attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, valid, acc, inv, a.d, half);
-    if (valid && half == 0) a.part_lse[split * rows + flat] = lse;
+    attn_store_rows<float, D>(a.part + (at.split * rows + flat) * a.d, valid, acc, inv, a.d, half);
+    if (valid && half == 0) a.part_lse[at.split * rows + flat] = lse;
+  }
+}
+
+// Single tokens are bound by reading K and V: in single precision they are multiplied as they are, on the fp32 instructions.
+template <typename T, int D> struct TokenTile {
+  static constexpr int kBytes = D * (int)sizeof(T), kPitch = kBytes + 16, kSteps = kBytes / 32, kPiece = 16 / sizeof(T);
+};
+template <typename T, int D> using TokenOwn = typename AttnPiece<T>::Type[TokenTile<T, D>::kSteps];
+
+template <int D>
+__device__ __forceinline__ void token_product(f32x16& x, const char* lds, const TokenOwn<_Float16, D>& own, int lane) {
+  const char* row = lds + (lane & 31) * TokenTile<_Float16, D>::kPitch + (lane >> 5) * 16;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(row + s * 32), own[s], x, 0, 0, 0);
+}
+template <int D>
+__device__ __forceinline__ void token_product(f32x16& x, const char* lds, const TokenOwn<float, D>& own, int lane) {
+  const char* row = lds + (lane & 31) * TokenTile<float, D>::kPitch + (lane >> 5) * 16;
+#pragma unroll
+  for (int s = 0; s < D / 8; ++s) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(row + s * 32);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], own[s][e], x, 0, 0, 0);
+  }
+}
+template <int D>
+__device__ __forceinline__ void token_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, _Float16) {
+  attn_product_t<D, 1>(acc, lds, x, lane);
+}
+template <int D>
+__device__ __forceinline__ void token_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, float) {
+  constexpr int kPitch = TokenTile<float, D>::kPitch;
+  const char* at = lds + 4 * (lane >> 5) * kPitch + (lane & 31) * 4;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+#pragma unroll
+    for (int blk = 0; blk < D / 32; ++blk)
+      acc[blk] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + (8 * (r / 4) + r % 4) * kPitch + blk * 128), x[r],
+                                                      acc[blk], 0, 0, 0);
   }
 }
 
@@ -137,7 +147,7 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
 // before the end.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) {
-  using Tile = AttnTile<T, D>;
+  using Tile = TokenTile<T, D>;
   constexpr int kBlock = 32 * Tile::kPitch;              // 32 keys or values of a wave
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
@@ -170,14 +180,18 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
 
   f32x16 acc[D / 32] = {};
   AttnRunning run;
-  AttnStage<T, D, 32, 64> stage_k, stage_v;
+  AttnStage<T, 32, Tile::kBytes, Tile::kPitch, 64> stage_k, stage_v;
   int t = begin + wave;
   if (t < end) {
-    stage_k.load(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
-    stage_v.load(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
+    stage_k.load_any(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
+    stage_v.load_any(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
   }
-  AttnOwn<T, D> q;
-  attn_load_own<T, D>(q, Q, valid, a.d, half);
+  TokenOwn<T, D> q;
+#pragma unroll
+  for (int s = 0; s < Tile::kSteps; ++s) {
+    q[s] = typename AttnPiece<T>::Type{};
+    if (valid) q[s] = attn_load_piece<T>(Q, (2 * s + half) * Tile::kPiece, a.d);
+  }
   if (a.scale < 0.f) {
 #pragma unroll
     for (int s = 0; s < Tile::kSteps; ++s) q[s] = -q[s];
@@ -207,15 +221,15 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     const int key0 = t * 32;
     t += kAttnWaves;
     if (t < end) {
-      stage_k.load(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
-      stage_v.load(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
+      stage_k.load_any(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
+      stage_v.load_any(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
     }
     unsigned word = ~0u;
     if (a.mask) word = valid ? (unsigned)(a.mask[lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 + row] >> (key0 & 32)) : 0u;
     word &= attn_low_bits(seen - key0);
     if (!__any(word != 0)) continue;
     f32x16 x[1] = {};
-    attn_product<D>(x[0], lds_k, q, lane);
+    token_product<D>(x[0], lds_k, q, lane);
     if (BIAS) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -224,15 +238,15 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
       }
     }
     if (__any(word != ~0u)) attn_hide(x[0], word, half);
-    attn_softmax_step<T, D, 1, BIAS>(x, run, acc, c);
-    attn_product_t<D>(acc, lds_v, x[0], lane, T{});
+    attn_softmax_step<D, 1, BIAS>(x, run, acc, c);
+    token_product_t<D>(acc, lds_v, x[0], lane, T{});
   }
 
   // the four waves' parts: each scaled to the common maximum, then added up in the waves' order
   __syncthreads();
   float* lds_acc = reinterpret_cast<float*>(lds_raw);                     // [4][32][D + 1]
   float* lds_stat = lds_acc + kAttnWaves * 32 * (D + 1);                  // [4][32][2]
-  const float sum = run.sum + attn_other_half(run.sum);
+  const float sum = attn_sum_halves(run.sum);
 #pragma unroll
   for (int blk = 0; blk < D / 32; ++blk)
 #pragma unroll
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
       value += v == v ? v * f : v;
     }
     const bool none = most == -__builtin_inff() && total == 0.f;
-    const float lse = none ? -__builtin_inff() : most * c * kLn2 + (__builtin_amdgcn_logf(total) - AttnType<T>::kOffset) * kLn2;
+    const float lse = none ? -__builtin_inff() : most * c * kLn2 + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
     const float result = none ? 0.f : value / total;
     const int64_t flat = ((int64_t)batch * a.heads + h) * a.m + i;
     if (a.splits == 1) {
@@ -307,25 +321,139 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[flat] = lse;
 }
 
-// Bits of the sparse matrix, from its CSR topology: cleared, then set by one wave per row.  Which of the threads sets a bit first
-// changes nothing.  Column indices out of range are passed over.
+// Bits of the sparse matrix, from its CSR topology: cleared, the words by rows set by one wave per row (which thread sets a bit first changes
+// nothing), then one wave per tile of 64 x 64 turns its 64 words by rows into 64 by columns and marks the tile.  Column indices out of
+// range are passed over.  (Setting the words by columns and the marks entry by entry, many threads at one word, took 5.8 ms for 1.7
+// million entries of 4096 x 4096.)
 __global__ __launch_bounds__(256) void attention_mask_clear_kernel(int64_t words, uint64_t* mask) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i < words) mask[i] = 0;
 }
-__global__ __launch_bounds__(256) void attention_mask_kernel(int m, int k, const int* __restrict__ row_offsets,
-                                                             const int* __restrict__ column_indices, unsigned long long* mask) {
+__global__ __launch_bounds__(256) void attention_mask_rows_kernel(int m, int k, const int* __restrict__ row_offsets,
+                                                                  const int* __restrict__ column_indices, unsigned long long* mask) {
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (row >= m) return;
   const MaskLayout lay(m, k);
-  const int64_t per_row = (lay.tj + 63) / 64, per_col = (lay.ti + 63) / 64;
   for (int p = row_offsets[row] + lane; p < row_offsets[row + 1]; p += kWave) {
     const int col = column_indices[p];
-    if (col < 0 || col >= k) continue;
-    atomicOr(mask + lay.row_words + (int64_t)(col >> 6) * lay.ti * 64 + row, 1ull << (col & 63));
-    atomicOr(mask + lay.col_words + (int64_t)(row >> 6) * lay.tj * 64 + col, 1ull << (row & 63));
-    atomicOr(mask + lay.row_tiles + (int64_t)(row >> 6) * per_row + (col >> 12), 1ull << ((col >> 6) & 63));
-    atomicOr(mask + lay.col_tiles + (int64_t)(col >> 6) * per_col + (row >> 12), 1ull << ((row >> 6) & 63));
+    if (col >= 0 && col < k) atomicOr(mask + lay.row_words + (int64_t)(col >> 6) * lay.ti * 64 + row, 1ull << (col & 63));
+  }
+}
+__global__ __launch_bounds__(256) void attention_mask_tiles_kernel(int m, int k, unsigned long long* mask) {
+  const MaskLayout lay(m, k);
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= lay.ti * lay.tj) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t ti = tile % lay.ti, tj = tile / lay.ti;
+  const unsigned long long word = mask[lay.row_words + (tj * lay.ti + ti) * 64 + lane];
+  if (!__any(word != 0)) return;                          // the words by columns are clear already
+  unsigned long long column = 0;
+#pragma unroll
+  for (int b = 0; b < 64; ++b) {
+    const unsigned long long rows = __ballot((word >> b) & 1);
+    if (lane == b) column = rows;
+  }
+  mask[lay.col_words + (ti * lay.tj + tj) * 64 + lane] = column;
+  if (lane == 0) {
+    atomicOr(mask + lay.row_tiles + ti * ((lay.tj + 63) / 64) + (tj >> 6), 1ull << (tj & 63));
+    atomicOr(mask + lay.col_tiles + tj * ((lay.ti + 63) / 64) + (ti >> 6), 1ull << (ti & 63));
+  }
+}
+
+// The largest finite number of each sequence's head of K and V (of Q, dO: of all heads that share one), in up to 64 parts.
+struct AttnOperand {
+  const void* from;
+  _Float16* to;
+  AttnStrides s;
+  int heads, group, rows;   // heads of K and V, and how many heads and rows of this operand belong to each
+  int keys;                 // whether its rows are states, of which `lengths` counts
+};
+struct AttnOperands {
+  AttnOperand of[4];
+  int count, batch, kv_heads, d, k, parts;
+  const int* lengths;
+  float *most, *factors;    // [batch * kv_heads][4][parts], [batch * kv_heads][4]
+};
+__device__ __forceinline__ int64_t attn_operand_rows(const AttnOperands& o, const AttnOperand& x, int batch) {
+  if (!x.keys) return (int64_t)x.group * x.rows;
+  return o.lengths ? min(max(o.lengths[batch], 0), x.rows) : x.rows;
+}
+template <typename T>
+__device__ __forceinline__ const T* attn_operand_row(const AttnOperand& x, int batch, int kv_head, int64_t r) {
+  const int g = (int)(r / x.rows);
+  return static_cast<const T*>(x.from) + batch * x.s.batch + ((int64_t)kv_head * x.group + g) * x.s.head + (r - (int64_t)g * x.rows) * x.s.row;
+}
+__global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperands o) {
+  __shared__ float waves[4];
+  int id = blockIdx.x;
+  const int part = id % o.parts;
+  id /= o.parts;
+  const int which = id % o.count;
+  id /= o.count;
+  const int kv_head = id % o.kv_heads, batch = id / o.kv_heads;
+  const AttnOperand& x = o.of[which];
+  const int64_t rows = attn_operand_rows(o, x, batch), begin = rows * part / o.parts, end = rows * (part + 1) / o.parts;
+  const int pieces = (o.d + 3) / 4;
+  float most = 0.f;
+  for (int64_t at = begin * pieces + threadIdx.x; at < end * pieces; at += 256) {
+    const int64_t r = at / pieces;
+    const f32x4 v = attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, r), (int)(at - r * pieces) * 4, o.d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float m = fabsf(v[e]);
+      most = m < __builtin_inff() ? fmaxf(most, m) : most;
+    }
+  }
+#pragma unroll
+  for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) o.most[(((int64_t)batch * o.kv_heads + kv_head) * 4 + which) * o.parts + part] = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+}
+// Copies of the operands for the panel kernels, rows of D numbers, zeros behind d and behind a sequence's states.  Single precision:
+// numbers times the power of two as two fp16 terms, the first ones of a row before the second ones.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands o, int64_t blocks_each) {
+  constexpr int kPieces = D / 8, kRows = 256 / kPieces;
+  const int64_t id = blockIdx.x / blocks_each, block = blockIdx.x - id * blocks_each;
+  const int which = (int)(id % o.count);
+  const int64_t bh = id / o.count;
+  const int kv_head = (int)(bh % o.kv_heads), batch = (int)(bh / o.kv_heads);
+  const AttnOperand& x = o.of[which];
+  const int64_t all = (int64_t)x.group * x.rows, rows = attn_operand_rows(o, x, batch);
+  const int64_t r = block * kRows + threadIdx.x / kPieces;
+  const bool mine = r < all && threadIdx.x < kRows * kPieces;
+  const int c = threadIdx.x % kPieces * 8;
+  _Float16* to = x.to + (bh * all + r) * (attn_terms<T>() * D) + c;
+  if constexpr (sizeof(T) == 2) {
+    f16x8 v = {};
+    if (mine && r < rows) v = attn_load_piece<_Float16>(attn_operand_row<_Float16>(x, batch, kv_head, r), c, o.d);
+    if (mine) *reinterpret_cast<f16x8*>(to) = v;
+  } else {
+    const int lane = threadIdx.x & 63;
+    float most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
+#pragma unroll
+    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+    const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
+    const float factor = ldexpf(1.f, e);
+    if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + which] = ldexpf(1.f, -e);
+    f16x8 hi = {}, lo = {};
+    if (mine && r < rows) {
+      const float* row = attn_operand_row<float>(x, batch, kv_head, r);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 v = attn_load_piece<float>(row, c + 4 * h, o.d) * factor;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          hi[4 * h + i] = (_Float16)v[i];
+          lo[4 * h + i] = (_Float16)(v[i] - (float)hi[4 * h + i]);
+        }
+      }
+    }
+    if (mine) {
+      *reinterpret_cast<f16x8*>(to) = hi;
+      *reinterpret_cast<f16x8*>(to + D) = lo;
+    }
   }
 }
 

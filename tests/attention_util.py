@@ -86,7 +86,10 @@ class Case:
         self.lengths, self.positions = ints(lengths), ints(positions)
         self.bucket_of = self.table = None
         if buckets:
-            self.bucket_of = torch.from_numpy(spdl.spdl_build_relative_buckets_host(buckets, span, both)).to(device)
+            # spans too short for the library's buckets: any bucket at each relative position
+            of = (spdl.spdl_build_relative_buckets_host(buckets, span, both) if span > buckets // 2 else
+                  np.random.default_rng(seed).integers(0, buckets, 2 * span + 1).astype(np.int32))
+            self.bucket_of = torch.from_numpy(of).to(device)
             self.table = torch.randn((heads, buckets), generator=gen).to(self.dt).to(device)
         self.seen = self.mask = None
         if mask is not None:

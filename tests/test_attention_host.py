@@ -124,7 +124,7 @@ def whole_number_bucket(rel, buckets, distance, both):
 
 
 @pytest.mark.parametrize("both", [True, False])
-@pytest.mark.parametrize("buckets,distance", [(32, 128), (16, 64), (64, 256), (128, 1024), (32, 20), (4, 2), (5, 100), (31, 1000), (33, 513)])
+@pytest.mark.parametrize("buckets,distance", [(32, 128), (16, 64), (64, 256), (128, 1024), (32, 20), (4, 3), (5, 100), (31, 1000), (33, 513)])
 def test_relative_buckets(buckets, distance, both):
     got = spdl.spdl_build_relative_buckets_host(buckets, distance, both)
     assert got.dtype == np.int32

@@ -46,7 +46,7 @@ def test_mask_with_lengths_and_shared_heads(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("buckets,span,both", [(4, 2, True), (2, 3, False), (32, 128, True), (32, 128, False), (128, 1024, True)])
+@pytest.mark.parametrize("buckets,span,both", [(3, 0, True), (3, 1, True), (20, 7, True), (2, 3, False), (32, 128, True), (32, 128, False), (128, 1024, True)])
 @pytest.mark.parametrize("m,k,positions", [(1, 300, [299, 7]), (16, 100, [-50, 400]), (150, 150, None), (260, 900, [100, -3]),
                                            (40, 64, [2 ** 31 - 1, -2 ** 31])])
 def test_bias(dtype, buckets, span, both, m, k, positions):
