@@ -18,7 +18,7 @@ constexpr int kMostWidth = 128;
 
 struct Plan {
   bool token;                          // the kernel for a few queries
-  int forward_splits, dq_splits, dkv_splits;
+  int forward_splits, dq_splits, dkv_splits, dbias_splits;
   int64_t forward_blocks, dq_blocks, dkv_blocks;      // without the splits
   int64_t rows, kv_rows, parts;        // parts: workgroups that leave sums of dS per head
   int width;                           // d rounded up to the width of a kernel
@@ -28,7 +28,7 @@ struct Plan {
   // offsets into the workspace, in bytes; the terms of Q, K, V and dO and their factors come first (single precision)
   int64_t most, factors, q16, k16, v16, g16;
   int64_t forward_part, part_lse, forward_bytes;
-  int64_t delta, part, row_sums, part_bias, backward_bytes;
+  int64_t delta, weight, ends, part, row_sums, part_bias, backward_bytes;
 };
 
 inline int kernel_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
@@ -67,7 +67,9 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, 4);
   x.dkv_blocks = (int64_t)p.batch * p.kv_heads * up(p.k, kAttnPanel);
   x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, 4);
-  x.parts = (int64_t)p.batch * up(p.m, kAttnPanel);
+  // tiles near the diagonal that a panel meets
+  x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 2);
+  x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dbias_splits;
   x.most_parts = (int)std::min<int64_t>(64, std::max<int64_t>(1, up(std::max<int64_t>(group * p.m, p.k), 64)));
 
   int64_t terms = 0, end = 0;
@@ -89,9 +91,11 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   end = terms;
   if (x.copied) x.g16 = take(end, x.rows * numbers);
   x.delta = take(end, x.rows);
+  x.weight = take(end, x.rows);
+  x.ends = take(end, 2 * x.rows);
   x.part = take(end, std::max(x.dq_splits > 1 ? x.dq_splits * x.rows * p.d : 0, x.dkv_splits > 1 ? 2 * x.dkv_splits * x.kv_rows * p.d : 0));
+  if (x.dq_splits > 1) x.row_sums = take(end, 2 * x.dq_splits * x.rows * kAttnRowSums);
   if (p.buckets > 0) {
-    x.row_sums = take(end, 2 * x.dq_splits * x.rows * 5);
     x.part_bias = take(end, x.parts * p.heads * (2 * (int64_t)p.span + 1));
   }
   x.backward_bytes = end;
@@ -149,7 +153,8 @@ AttnArgs make_args(const spdl_attention_problem& p, const void* Q, const void* K
   return a;
 }
 
-bool launch(void (*kernel)(AttnArgs), int64_t blocks, int lds, const AttnArgs& a, hipStream_t stream) {
+bool launch(void (*kernel)(AttnArgs), int64_t blocks, int lds, AttnArgs a, hipStream_t stream) {
+  a.by_length = a.lengths && a.batch > 1 && a.batch <= 64;
   if (lds > 64 * 1024 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return false;
@@ -185,7 +190,10 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
   o.batch = a.batch, o.kv_heads = a.kv_heads, o.d = a.d, o.k = a.k, o.parts = x.most_parts, o.lengths = a.lengths;
   o.most = reinterpret_cast<float*>(w + x.most), o.factors = reinterpret_cast<float*>(w + x.factors);
   const int64_t each = (int64_t)a.batch * a.kv_heads * o.count;
-  if (sizeof(T) == 4) {
+  // up to 2^13 numbers of a head every wave looks for the largest itself
+  if (std::max<int64_t>((int64_t)a.group * a.m, a.k) * a.d <= 8192) {
+    o.most = nullptr;
+  } else if (sizeof(T) == 4) {
     attention_largest_kernel<<<dim3((unsigned)(each * o.parts)), dim3(256), 0, stream>>>(o);
     if (hipGetLastError() != hipSuccess) return false;
   }
@@ -211,29 +219,33 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   using Tile = AttnTile<D, attn_terms<T>()>;
   constexpr int kTiles = Tile::kSets * Tile::kPair;
   const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
+  const int64_t pieces = up(a.d, 4);
   float* part = a.part = reinterpret_cast<float*>(w + x.part);
   if ((x.dq_blocks > 0 || x.dkv_blocks > 0) && !prepare_operands<T, D>(x, a, w, true, stream)) return false;
   if (x.dq_blocks > 0) {
     a.splits = x.dq_splits;
     if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, kTiles + bias, a, stream)) return false;
     if (a.splits > 1) {
-      attention_sum_kernel<T><<<dim3((unsigned)up(x.rows * a.d, 256)), dim3(256), 0, stream>>>(a.splits, x.rows, a.heads, a.m, a.d, part,
-                                                                                              AttnSum{a.dq, a.dQ}, AttnSum{});
+      if (attn_row_sums<T, BIAS>()) {
+        attention_rows_kernel<T, BIAS><<<dim3((unsigned)up(x.rows, 256)), dim3(256), 0, stream>>>(a);
+        if (hipGetLastError() != hipSuccess) return false;
+      }
+      attention_sum_kernel<T><<<dim3((unsigned)up(x.rows * pieces, 256)), dim3(256), 0, stream>>>(
+          a.splits, x.rows, a.heads, a.m, a.d, part, sizeof(T) == 4 ? a.weight : nullptr, AttnSum{a.dq, a.dQ}, AttnSum{});
       if (hipGetLastError() != hipSuccess) return false;
     }
     if (BIAS && a.part_bias) {
-      a.row_splits = a.splits;
-      a.splits = 1;
+      a.splits = x.dbias_splits;
       const int lds = kTiles + bias + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
-      if (!launch(attention_dbias_kernel<T, D>, x.dq_blocks, lds, a, stream)) return false;
+      if (!launch(attention_dbias_kernel<T, D>, x.dq_blocks * a.splits, lds, a, stream)) return false;
     }
   }
   if (x.dkv_blocks > 0) {
     a.splits = x.dkv_splits;
-    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 2 * kAttnTile * 4 + bias, a, stream)) return false;
+    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 3 * kAttnTile * 4 + bias, a, stream)) return false;
     if (a.splits > 1) {
-      attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * a.d, 256)), dim3(256), 0, stream>>>(
-          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
+      attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(
+          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, nullptr, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
       if (hipGetLastError() != hipSuccess) return false;
     }
   }
@@ -280,7 +292,7 @@ int attention(const spdl_attention_problem* p, const void* Q, const void* K, con
   (void)hipGetLastError();
   if (!(table ? dispatch_forward<T, true>(x, a, w, s) : dispatch_forward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (a.splits > 1) {
-    attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 4)), dim3(256), 0, s>>>(a);
+    attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 16)), dim3(256), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   }
   return SPDL_OK;
@@ -307,7 +319,9 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   a.dO = dO, a.dQ = dQ, a.dK = dK, a.dV = dV;
   char* w = static_cast<char*>(workspace);
   a.delta = reinterpret_cast<float*>(w + x.delta);
-  a.row_sums = dtable ? reinterpret_cast<double*>(w + x.row_sums) : nullptr;
+  a.weight = reinterpret_cast<float*>(w + x.weight);
+  a.ends = reinterpret_cast<float*>(w + x.ends);
+  a.row_sums = reinterpret_cast<double*>(w + x.row_sums);
   a.part_bias = dtable ? reinterpret_cast<float*>(w + x.part_bias) : nullptr;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();

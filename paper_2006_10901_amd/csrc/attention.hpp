@@ -37,7 +37,7 @@ struct AttnStrides { int64_t batch, head, row; };
 // What a call hands to the kernels.  mask_*: bits of the sparse matrix (see MaskLayout).
 struct AttnArgs {
   int batch, heads, kv_heads, group, m, k, d;
-  int span, buckets, splits, row_splits;
+  int span, buckets, splits, by_length;
   float scale;
   AttnStrides q, kk, v, o, dout, dq, dk, dv;
   const void *Q, *K, *V, *dO;
@@ -53,10 +53,12 @@ struct AttnArgs {
   void* O;
   float* lse;
   void *dQ, *dK, *dV;
-  float* delta;          // workspace, [batch, heads, m]
+  float* delta;          // workspace, of each row: D, what its weights are taken times, the sums of dS at the bias's ends
+  float* weight;
+  float* ends;
   float* part;           // workspace: what splits leave for the join
   float* part_lse;
-  double* row_sums;      // workspace: of every row and split, sums that the gradient of the bias needs (see attention_dq_kernel)
+  double* row_sums;      // workspace: of every split and row, the sums over its keys
   float* part_bias;      // workspace: sums of dS by relative position, one set of 2 span + 1 per panel
 };
 
@@ -311,33 +313,59 @@ __device__ __forceinline__ int attn_position(const AttnArgs& a, int batch) {
   return a.positions ? min(max(a.positions[batch], -(1 << 30)), 1 << 30) : 0;
 }
 
-// Runs of neighbouring pieces of work go to one XCD, whose L2 then keeps the K and V (or Q and dO) that they share: workgroup ids are
-// dealt to the eight XCDs in turn.
-__device__ __forceinline__ int attn_work(int id, int total) {
-  const int xcd = id & 7, each = total >> 3, rest = total & 7;
-  return xcd * each + min(xcd, rest) + (id >> 3);
-}
-
 template <typename T> constexpr int attn_terms() { return sizeof(T) == 4 ? 2 : 1; }
 
 // How many of its states a sequence has.
 __device__ __forceinline__ int attn_seen(const AttnArgs& a, int batch) { return a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k; }
+
+// Which sequence and head of K and V a workgroup works for, and which of the `inner` pieces of work that each has.  Runs of neighbouring
+// pieces go to one XCD, whose L2 then keeps the K and V (or Q and dO) that they share: workgroup ids are dealt to the eight XCDs in turn.
+//
+// Sequences of unequal length (by_length: lengths known, at most 64 of them): an XCD still gets whole heads where their number allows, and
+// takes the longest sequences first.  Workgroups that start together go to the compute units in turn, 32 of an XCD, and those that meet on
+// one share it, so every other 32 are taken from the back: the longest is met by the shortest.  (Eight sequences of a quarter to all of 2048 states, 16
+// heads, 512 queries, fp16: MEASURED.)
+struct AttnPlace {
+  int batch, kv_head, piece;
+  __device__ __forceinline__ AttnPlace(const AttnArgs& a, int inner) {
+    const int id = blockIdx.x, total = gridDim.x, xcd = id & 7;
+    if (!a.by_length) {
+      const int each = total >> 3, rest = total & 7;
+      int work = xcd * each + min(xcd, rest) + (id >> 3);
+      piece = work % inner;
+      work /= inner;
+      batch = work % a.batch;
+      kv_head = work / a.batch;
+      return;
+    }
+    const bool own = a.kv_heads % 8 == 0;                 // heads of its own for each XCD
+    const int at = own ? id >> 3 : id, all = own ? total >> 3 : total, units = own ? 32 : 256, heads = own ? a.kv_heads >> 3 : a.kv_heads;
+    const int turn = at / units, slot = at - turn * units, count = min(units, all - turn * units);
+    int work = turn * units + (turn & 1 ? count - 1 - slot : slot);
+    piece = work % inner;
+    work /= inner;
+    kv_head = (own ? xcd * heads : 0) + work % heads;
+    const int want = work / heads, lane = threadIdx.x & 63, mine = lane < a.batch ? a.lengths[lane] : INT32_MIN;
+    int rank = 0;
+    for (int i = 0; i < a.batch; ++i) {
+      const int other = __builtin_amdgcn_readlane(mine, i);
+      rank += other > mine || (other == mine && i < lane);
+    }
+    batch = uniform(__builtin_ctzll(__ballot(lane < a.batch && rank == want)));
+  }
+};
 
 // The panel of 128 queries that a workgroup works on, and which part of the keys.
 struct AttnPanelOf {
   int split, panel, batch, kv_head, head, panels;
   __device__ __forceinline__ AttnPanelOf(const AttnArgs& a, int rows) {
     panels = (rows + kAttnPanel - 1) / kAttnPanel;
-    int work = attn_work(blockIdx.x, gridDim.x);
-    split = work % a.splits;
-    work /= a.splits;
-    panel = work % panels;
-    work /= panels;
-    const int of_group = work % a.group;
-    work /= a.group;
-    batch = work % a.batch;
-    kv_head = work / a.batch;
-    head = kv_head * a.group + of_group;
+    const AttnPlace at(a, a.group * panels * a.splits);
+    batch = at.batch, kv_head = at.kv_head;
+    split = at.piece % a.splits;
+    const int rest = at.piece / a.splits;
+    panel = rest % panels;
+    head = kv_head * a.group + rest / panels;
   }
 };
 __device__ __forceinline__ void attn_tiles_of_split(const AttnArgs& a, int split, int seen, int& begin, int& end) {

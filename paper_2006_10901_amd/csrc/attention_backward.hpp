@@ -37,10 +37,43 @@ struct AttnScale {
 // Whether all relative positions of a block of 32 x 32 lie at the clamped ends of a bias; near: that of its first key and first query.
 __device__ __forceinline__ bool attn_far(int near, int span) { return near - 31 >= span || near + 31 <= -span; }
 
-// What a row leaves for the gradient of the bias: the sum of all dS (0, but for the error of D), and those of dS and P over the
-// blocks that lie at the lower and at the upper end.
-// Added up in 64 bits: sums of thousands of terms that nearly cancel.
-struct AttnRowSums { double all, low, low_p, high, high_p; };
+// What a pass over a row's keys tells of the row: the sums of dS and of P over all of them and, for the gradient of the bias, over the
+// blocks that lie at its lower and at its upper end.  Added up in 64 bits: sums of thousands of terms that nearly cancel.
+//
+// P comes from lse, which is rounded to 2^-24 of itself: an error of up to 5e-7 that all weights of a row share.  D is off by
+// what rounding O cost.  But P adds up to 1 over a row, and dS to 0, so that the sums tell both errors: weights are P / sum P, and D
+// is right once sum dS / sum P is added.  (Single precision: 9.2e-7 -> 4.7e-7 of dK's 2-norm.  Half precision with a bias: dtable's sums
+// nearly cancel and were off by 3.8e-4 .. 1.2e-3, now 1.7e-4, what rounding the result costs.)
+struct AttnRowSums { double ds, p, low, low_p, high, high_p; };
+constexpr int kAttnRowSums = 6;
+// Whether a call needs them, and the weights' part of it.
+template <typename T, bool BIAS> constexpr bool attn_row_sums() { return BIAS || sizeof(T) == 4; }
+
+// What the other kernels take of a row: D, 1 / sum P (single precision) and the sums of dS at the ends.
+template <typename T, bool BIAS>
+__device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat, float delta, const AttnRowSums& s) {
+  const bool any = s.p > 0. && s.p < 1e30;                // not a row that sees nothing, nor one of Inf or NaN
+  const double weight = any ? 1. / s.p : 1., more = any ? s.ds * weight : 0.;
+  a.delta[flat] = (float)(delta + more);
+  if constexpr (sizeof(T) == 4) a.weight[flat] = (float)weight;
+  if constexpr (BIAS) {
+    const double f = sizeof(T) == 4 ? weight : 1.;
+    a.ends[2 * flat] = (float)(f * (s.low - more * s.low_p));
+    a.ends[2 * flat + 1] = (float)(f * (s.high - more * s.high_p));
+  }
+}
+template <typename T, bool BIAS>
+__global__ __launch_bounds__(256) void attention_rows_kernel(const AttnArgs a) {
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (flat >= rows) return;
+  AttnRowSums s = {};
+  for (int i = 0; i < a.splits; ++i) {
+    const double* from = a.row_sums + (i * rows + flat) * kAttnRowSums;
+    s.ds += from[0], s.p += from[1];
+    if (BIAS) s.low += from[2], s.low_p += from[3], s.high += from[4], s.high_p += from[5];
+  }
+  attn_finish_row<T, BIAS>(a, flat, a.delta[flat], s);
+}
 
 // A workgroup's panel of queries for the backward pass.
 template <typename T, int D, bool BIAS> struct AttnQueries {
@@ -70,6 +103,7 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
+  constexpr bool kSums = attn_row_sums<T, BIAS>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
@@ -106,7 +140,6 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
     }
   }
   delta = attn_sum_halves(delta);
-  if (valid && half == 0 && at.split == 0) a.delta[own.flat] = delta;
 
   const MaskLayout lay(a.m, a.k);
   const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
@@ -160,14 +193,15 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
         if (hide) p = attn_bit(w, r) ? p : 0.f;
         x[r] = p * __builtin_fmaf(y[r], own.to_dp, -delta);
         if (hide) x[r] = attn_bit(w, r) ? x[r] : 0.f;      // whatever stands where the row does not look
-        if (BIAS) {
+        if (kSums) {
           sum += x[r];
           sum_p += p;
         }
       }
-      if (BIAS) {
-        sums.all += sum;
-        if (far) {
+      if (kSums) {
+        sums.ds += sum;
+        sums.p += sum_p;
+        if (BIAS && far) {
           (near > 0 ? sums.high : sums.low) += sum;
           (near > 0 ? sums.high_p : sums.low_p) += sum_p;
         }
@@ -177,22 +211,31 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
     }
   }
 
-  const float factor = a.scale * f.k / ds_scale.factor;
+  float factor = a.scale * f.k / ds_scale.factor;
   const int64_t rows = (int64_t)a.batch * a.heads * a.m;
+  if constexpr (kSums) {
+    double s[kAttnRowSums] = {sums.ds, sums.p, sums.low, sums.low_p, sums.high, sums.high_p};
+#pragma unroll
+    for (int i = 0; i < kAttnRowSums; ++i) s[i] += __shfl_xor(s[i], 32);
+    const AttnRowSums all = {s[0], s[1], s[2], s[3], s[4], s[5]};
+    if (a.splits == 1) {
+      if (sizeof(T) == 4 && all.p > 0. && all.p < 1e30) factor *= (float)(1. / all.p);
+      if (valid && half == 0) attn_finish_row<T, BIAS>(a, own.flat, delta, all);
+    } else if (valid && half == 0) {
+      if (at.split == 0) a.delta[own.flat] = delta;
+      double* to = a.row_sums + (at.split * rows + own.flat) * kAttnRowSums;
+#pragma unroll
+      for (int i = 0; i < kAttnRowSums; ++i)
+        if (BIAS || i < 2) to[i] = s[i];
+    }
+  } else if (valid && half == 0 && at.split == 0) {
+    a.delta[own.flat] = delta;
+  }
   if (a.splits == 1) {
     T* dQ = static_cast<T*>(a.dQ) + batch * a.dq.batch + head * a.dq.head + (int64_t)row * a.dq.row;
     attn_store_rows<T, D>(dQ, valid, acc, factor, a.d, half);
   } else {
     attn_store_rows<float, D>(a.part + (at.split * rows + own.flat) * a.d, valid, acc, factor, a.d, half);
-  }
-  if (BIAS && a.row_sums) {
-    double* to = a.row_sums + (at.split * rows + own.flat) * 5;
-    double s[5] = {sums.all, sums.low, sums.low_p, sums.high, sums.high_p};
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      s[i] += __shfl_xor(s[i], 32);
-      if (valid && half == 0) to[i] = s[i];
-    }
   }
 }
 
@@ -225,10 +268,8 @@ __device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block
 
 constexpr int kAttnDiagonalBlock = 32 * 33;               // floats per wave
 
-// The gradient of the bias by relative position, by panels of 128 queries.  In half precision D is off by what rounding O cost, by as
-// much as a bucket's sum of dS, whose terms nearly cancel, is off; but over a row dS adds up to 0, so that the sum that it gave with that
-// D is D's error, and dS less that times P is right.  Where relative positions lie at the ends of the bias, the sums that
-// attention_dq_kernel left of each row are put right so; the blocks near the diagonal are formed again with the right D.
+// The gradient of the bias by relative position, by panels of 128 queries: the blocks near the diagonal are formed again, with the
+// right D; what lies at the ends of the bias attention_dq_kernel has summed by rows.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
@@ -240,7 +281,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   const int n = 2 * a.span + 1;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
-  const AttnPanelOf at(a, a.m);                           // a.splits is 1 here, row_splits those that left row_sums
+  const AttnPanelOf at(a, a.m);
   const int batch = at.batch, head = at.head, kv_head = at.kv_head;
   const int seen = attn_seen(a, batch);
   const int first_row = at.panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
@@ -248,7 +289,8 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   const int position = attn_position(a, batch);
   // tiles that hold relative positions between the ends
   const int lowest = position + first_row - a.span - kAttnTile, highest = position + first_row + kAttnPanel + a.span;
-  const int begin = max(lowest, 0) / kAttnTile, end = min((seen + kAttnTile - 1) / kAttnTile, max(highest, 0) / kAttnTile + 1);
+  const int from = max(lowest, 0) / kAttnTile, to = max(from, min((seen + kAttnTile - 1) / kAttnTile, max(highest, 0) / kAttnTile + 1));
+  const int begin = from + (to - from) * at.split / a.splits, end = from + (to - from) * (at.split + 1) / a.splits;
 
   const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
   const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
@@ -259,17 +301,12 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   float* sums = lds_sums + wave * n;
   for (int x = lane; x < n; x += 64) sums[x] = 0.f;
 
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
-  float delta = 0.f;
+  float delta = 0.f, weight = 1.f;
   double low = 0., high = 0.;
   if (valid) {
-    AttnRowSums s = {};
-    for (int i = 0; i < a.row_splits; ++i) {
-      const double* from = a.row_sums + (i * rows + own.flat) * 5;
-      s.all += from[0], s.low += from[1], s.low_p += from[2], s.high += from[3], s.high_p += from[4];
-    }
-    delta = (float)(a.delta[own.flat] + s.all);
-    if (half == 0) low = s.low - s.all * s.low_p, high = s.high - s.all * s.high_p;
+    delta = a.delta[own.flat];
+    if (sizeof(T) == 4) weight = a.weight[own.flat];
+    if (half == 0 && at.split == 0) low = a.ends[2 * own.flat], high = a.ends[2 * own.flat + 1];
   }
 
   const MaskLayout lay(a.m, a.k);
@@ -304,7 +341,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
       attn_add_bias<1>(x, own.scale, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? own.weight(x[r]) * __builtin_fmaf(y[r], own.to_dp, -delta) : 0.f;
+      for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? own.weight(x[r]) * weight * __builtin_fmaf(y[r], own.to_dp, -delta) : 0.f;
       attn_sum_diagonals(x, lds_blocks + wave * kAttnDiagonalBlock, sums, near, a.span, low, high, lane);
     }
   }
@@ -318,12 +355,12 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
     sums[2 * a.span] += (float)high;
   }
   __syncthreads();
-  float* to = a.part_bias + (((int64_t)head * a.batch + batch) * at.panels + at.panel) * n;
+  float* sum_to = a.part_bias + ((((int64_t)head * a.batch + batch) * at.panels + at.panel) * a.splits + at.split) * n;
   for (int x = tid; x < n; x += 256) {
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) s += lds_sums[w * n + x];
-    to[x] = s;
+    sum_to[x] = s;
   }
 }
 
@@ -333,17 +370,13 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set: 64 times lse, 64 times D
-  float* lds_bias = lds_stats + Tile::kSets * 2 * kAttnTile;
+  float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set: 64 times lse, D and what P is taken times
+  float* lds_bias = lds_stats + Tile::kSets * 3 * kAttnTile;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
   const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
-  int work = attn_work(blockIdx.x, gridDim.x);
-  const int split = work % a.splits;
-  work /= a.splits;
-  const int panel = work % panels;
-  work /= panels;
-  const int batch = work % a.batch, kv_head = work / a.batch;
+  const AttnPlace place(a, panels * a.splits);
+  const int split = place.piece % a.splits, panel = place.piece / a.splits, batch = place.batch, kv_head = place.kv_head;
 
   const int seen = attn_seen(a, batch);
   const int first_key = panel * kAttnPanel, wave_key = first_key + wave * 32, key = wave_key + (lane & 31);
@@ -392,7 +425,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
     stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, tid);
     stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, tid);
     const int r = tid & 63;
-    if (tid < 128) stat = r < rows ? (tid < 64 ? a.lse : a.delta)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
+    if (tid < (kTerms == 2 ? 192 : 128))
+      stat = r < rows ? (tid < 64 ? a.lse : tid < 128 ? a.delta : a.weight)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
   };
   int64_t at = next(begin);
   int bias_head = -1;
@@ -400,8 +434,9 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   for (int set = 0; at < end; set ^= Tile::kSets - 1) {
     char* lds_q = lds_raw + set * Tile::kPair;
     char* lds_g = lds_q + kAttnTile * Tile::kPitch;
-    float* lds_lse = lds_stats + set * 2 * kAttnTile;
+    float* lds_lse = lds_stats + set * 3 * kAttnTile;
     float* lds_delta = lds_lse + kAttnTile;
+    float* lds_weight = lds_delta + kAttnTile;
     if (Tile::kSets == 1) __syncthreads();
     stage_q.store(lds_q, tid);
     stage_g.store(lds_g, tid);
@@ -410,8 +445,8 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
       // rows that see nothing, and those behind the last, have no weights
       const float l = stat == -__builtin_inff() ? __builtin_inff() : stat;
       lds_lse[tid] = BIAS ? l : kOffset - l * kLog2e;
-    } else if (tid < 128) {
-      lds_delta[tid - 64] = stat;
+    } else if (tid < (kTerms == 2 ? 192 : 128)) {
+      lds_lse[tid] = stat;
     }
     const uint64_t word = valid ? word_next : 0ull;
     if (BIAS && h != bias_head) {
@@ -439,10 +474,13 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
       for (int q4 = 0; q4 < 4; ++q4) {
         const f32x4 l = *reinterpret_cast<const f32x4*>(lds_lse + b * 32 + q4 * 8 + half * 4);
         const f32x4 dl = *reinterpret_cast<const f32x4*>(lds_delta + b * 32 + q4 * 8 + half * 4);
+        f32x4 wt = {};
+        if constexpr (kTerms == 2) wt = *reinterpret_cast<const f32x4*>(lds_weight + b * 32 + q4 * 8 + half * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * q4 + e;
           float p = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[r] - l[e], c, kOffset)) : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, l[e]));
+          if constexpr (kTerms == 2) p *= wt[e];
           float s = p * __builtin_fmaf(y[r], to_dp, -dl[e]);
           if (hide) {
             p = attn_bit(w, r) ? p : 0.f;
@@ -473,25 +511,29 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   }
 }
 
-// Adds up what `splits` workgroups left of each of the rows, in their order: of one array, or of two that lie one behind the other.
+// Adds up what `splits` workgroups left of each of the rows, in their order: of one array, or of two that lie one behind the other; a
+// thread has four neighbouring elements of a row.  weight: what a row is taken times, or null.
 struct AttnSum { AttnStrides to; void* out; };
 template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part, AttnSum first,
-                                                            AttnSum second) {
-  int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const bool behind = at >= rows * d;
-  if (behind) {
-    at -= rows * d;
-    part += splits * rows * d;
-  }
+__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part,
+                                                            const float* weight, AttnSum first, AttnSum second) {
+  const int pieces = (d + 3) / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = rows * pieces;
+  const bool behind = at >= all;
+  if (behind) part += splits * rows * d;
   const AttnSum& x = behind ? second : first;
-  if (at >= rows * d || !x.out) return;
-  const int64_t flat = at / d;
-  const int col = (int)(at - flat * d);
-  float s = 0.f;
-  for (int i = 0; i < splits; ++i) s += part[(int64_t)i * rows * d + at];
+  if (at >= 2 * all || !x.out) return;
+  const int64_t flat = (behind ? at - all : at) / pieces;
+  const int c = (int)((behind ? at - all : at) - flat * pieces) * 4;
+  f32x4 s = {};
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i) s += attn_load_piece<float>(part + (i * rows + flat) * d, c, d);
+  if (weight) s *= weight[flat];
   const int64_t bh = flat / per_head;
-  static_cast<T*>(x.out)[bh / heads * x.to.batch + bh % heads * x.to.head + (flat % per_head) * x.to.row + col] = (T)s;
+  T* row = static_cast<T*>(x.out) + bh / heads * x.to.batch + bh % heads * x.to.head + (flat % per_head) * x.to.row;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (c + e < d) row[c + e] = (T)s[e];
 }
 
 // dtable of one head: the panels' sums by relative position (sixteen waves take panels in turn, then are added up in their order), then

@@ -199,7 +199,8 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
   const float scale = fabsf(a.scale);
   const float c = BIAS ? kLog2e : fmaxf(scale * kLog2e, 1e-37f);
   const MaskLayout lay(a.m, a.k);
-  int position = 0;
+  int position = 0, first = 0;
+  float low = 0.f, high = 0.f;                           // the bias at its ends
   const float* table = nullptr;
   if (BIAS) {
     const int head0 = panel * 32 / a.m;                  // of the group, the first one in this panel
@@ -208,8 +209,10 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     for (int x = tid; x < heads * a.buckets; x += 256) lds_table[x] = (float)from[x];
     for (int x = tid; x < 2 * a.span + 1; x += 256) lds_bucket[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
     table = lds_table + (valid ? of_group - head0 : 0) * a.buckets;
-    position = attn_position(a, batch) + row;
+    first = attn_position(a, batch);
+    position = first + row;
     __syncthreads();
+    low = table[lds_bucket[0]], high = table[lds_bucket[2 * a.span]];
   }
   while (t < end) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -230,7 +233,9 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     if (!__any(word != 0)) continue;
     f32x16 x[1] = {};
     token_product<D>(x[0], lds_k, q, lane);
-    if (BIAS) {
+    if (BIAS && (key0 - (first + a.m - 1) >= a.span || key0 + 31 - first <= -a.span)) {
+      attn_add_constant(x[0], scale, key0 > first ? high : low);
+    } else if (BIAS) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int rel = key0 + 8 * (r / 4) + 4 * half + r % 4 - position;
@@ -289,34 +294,45 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
   }
 }
 
-// Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s, in the parts' order.  A wave per row.
+// Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s, in the parts' order.  16 lanes per row, four neighbouring
+// elements each.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
-  const int64_t flat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   if (flat >= rows) return;
-  const int lane = threadIdx.x & 63;
-  float most = -__builtin_inff();
-  bool nan = false;
-  for (int s = 0; s < a.splits; ++s) {
+  const int lane = threadIdx.x & 15;
+  float most = -__builtin_inff(), nan = 0.f;
+  for (int s = lane; s < a.splits; s += 16) {
     const float l = a.part_lse[s * rows + flat];
-    nan |= l != l;
+    nan += l != l ? 1.f : 0.f;
     most = fmaxf(most, l);
   }
+#pragma unroll
+  for (int i = 1; i < 16; i <<= 1) {
+    most = fmaxf(most, __shfl_xor(most, i));
+    nan += __shfl_xor(nan, i);
+  }
   float total = 0.f;
-  for (int s = 0; s < a.splits && most != -__builtin_inff(); ++s) total += __builtin_amdgcn_exp2f((a.part_lse[s * rows + flat] - most) * kLog2e);
-  const float lse = nan ? __builtin_nanf("") : most == -__builtin_inff() ? most : most + __builtin_amdgcn_logf(total) * kLn2;
+  for (int s = lane; s < a.splits && most != -__builtin_inff(); s += 16) total += __builtin_amdgcn_exp2f((a.part_lse[s * rows + flat] - most) * kLog2e);
+#pragma unroll
+  for (int i = 1; i < 16; i <<= 1) total += __shfl_xor(total, i);
+  const float lse = nan > 0.f ? __builtin_nanf("") : most == -__builtin_inff() ? most : most + __builtin_amdgcn_logf(total) * kLn2;
   const int i = (int)(flat % a.m);
   const int64_t bh = flat / a.m;
   const int h = (int)(bh % a.heads);
   T* O = static_cast<T*>(a.O) + bh / a.heads * a.o.batch + h * a.o.head + (int64_t)i * a.o.row;
-  for (int col = lane; col < a.d; col += 64) {
-    float value = 0.f;
+  for (int c = lane * 4; c < a.d; c += 64) {
+    f32x4 value = {};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) {
       const float l = a.part_lse[s * rows + flat];
-      if (l != -__builtin_inff()) value = __builtin_fmaf(__builtin_amdgcn_exp2f((l - lse) * kLog2e), a.part[(s * rows + flat) * a.d + col], value);
+      const f32x4 v = attn_load_piece<float>(a.part + (s * rows + flat) * a.d, c, a.d);
+      const float f = __builtin_amdgcn_exp2f((l - lse) * kLog2e);
+      if (l != -__builtin_inff()) value += f * v;
     }
-    O[col] = (T)value;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < a.d) O[c + e] = (T)value[e];
   }
   if (lane == 0 && a.lse) a.lse[flat] = lse;
 }
@@ -383,6 +399,14 @@ __device__ __forceinline__ const T* attn_operand_row(const AttnOperand& x, int b
   const int g = (int)(r / x.rows);
   return static_cast<const T*>(x.from) + batch * x.s.batch + ((int64_t)kv_head * x.group + g) * x.s.head + (r - (int64_t)g * x.rows) * x.s.row;
 }
+__device__ __forceinline__ float attn_largest(float most, const f32x4& v) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float m = fabsf(v[e]);
+    most = m < __builtin_inff() ? fmaxf(most, m) : most;
+  }
+  return most;
+}
 __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperands o) {
   __shared__ float waves[4];
   int id = blockIdx.x;
@@ -397,12 +421,7 @@ __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperan
   float most = 0.f;
   for (int64_t at = begin * pieces + threadIdx.x; at < end * pieces; at += 256) {
     const int64_t r = at / pieces;
-    const f32x4 v = attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, r), (int)(at - r * pieces) * 4, o.d);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float m = fabsf(v[e]);
-      most = m < __builtin_inff() ? fmaxf(most, m) : most;
-    }
+    most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, r), (int)(at - r * pieces) * 4, o.d));
   }
 #pragma unroll
   for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
@@ -431,7 +450,17 @@ __global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands
     if (mine) *reinterpret_cast<f16x8*>(to) = v;
   } else {
     const int lane = threadIdx.x & 63;
-    float most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
+    float most = 0.f;
+    if (o.most) {
+      most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
+    } else {                                              // few numbers: every wave looks at all of them
+      const int pieces = (o.d + 3) / 4;
+#pragma unroll 4
+      for (int64_t at = lane; at < rows * pieces; at += 64) {
+        const int64_t row = at / pieces;
+        most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, row), (int)(at - row * pieces) * 4, o.d));
+      }
+    }
 #pragma unroll
     for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
     const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
