@@ -242,7 +242,7 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   }
   if (x.dkv_blocks > 0) {
     a.splits = x.dkv_splits;
-    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 3 * kAttnTile * 4 + bias, a, stream)) return false;
+    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 5 * kAttnTile * 4 + bias, a, stream)) return false;
     if (a.splits > 1) {
       attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(
           a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, nullptr, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});

@@ -277,9 +277,6 @@ __device__ __forceinline__ void attn_store_rows(T* row, bool valid, const f32x16
     }
 }
 
-// Which bit of a word belongs to register r of a lane in half h: bit 8 (r / 4) + r % 4 of the word shifted by 4 h.
-__device__ __forceinline__ bool attn_bit(unsigned word, int r) { return (word >> (8 * (r / 4) + r % 4)) & 1u; }
-
 __device__ __forceinline__ unsigned attn_low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // The next tile from `t` on (below `end`) in which a set of rows sees anything; `a`, `b`: two sets of bits of tiles (both count), or null.
@@ -414,47 +411,70 @@ __device__ __forceinline__ void attn_add_constant(f32x16& x, float scale, float 
 // One row's running softmax: columns of 32 x 32 scores in 16 registers, two lanes to a column.
 struct AttnRunning { float most = -__builtin_inff(), sum = 0.f; };
 
-// x: NB blocks of scores, as the product left them (BIAS: scaled and biased already); turns them into weights relative to the
-// running maximum and scales what has been summed before.  c: what the exponent is multiplied by to be one of 2.
-template <int D, int NB, bool BIAS>
-__device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& run, f32x16 (&acc)[D / 32], float c) {
+// How the scores of a tile come from products: s = scale x + bias.  Where one bias goes for all of them (no bias, or a tile at one end of
+// it) it takes one instruction per score to be the exponent of a weight.  Where each has its own, or the one is so large that scores
+// are lost in it (and have to be, as in any sum of the two), the scores are formed first: three.
+constexpr float kAttnLargeBias = 1e6f;
+struct AttnScores { float scale; bool formed; float bias; };
+
+// x: NB blocks of products (AttnScores::formed: of scores); turns them into weights relative to the running maximum and scales what has
+// been summed before.
+template <int D, int NB>
+__device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& run, f32x16 (&acc)[D / 32], const AttnScores& how) {
   float most = -__builtin_inff();
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) most = fmaxf(most, x[b][r]);
   most = attn_max_halves(most);
+  if (!how.formed) most = __builtin_fmaf(most, how.scale, how.bias);
   if (__any(most > run.most)) {
     asm volatile("");
     const float now = fmaxf(run.most, most);
     // a column that has seen nothing yet has nothing to be scaled: its factor is 0, and (-inf) - (-inf) is not formed
-    const float factor = run.most == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((run.most - now) * c);
+    const float factor = run.most == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((run.most - now) * kLog2e);
     run.sum *= factor;
 #pragma unroll
     for (int blk = 0; blk < D / 32; ++blk) acc[blk] *= factor;
     run.most = now;
   }
   const float base = run.most == -__builtin_inff() ? 0.f : run.most;
-  // Scores of a bias are subtracted first: a bias of the type's lowest value times log2 e would be an infinity.
-  const float shift = BIAS ? base : kOffset - base * c;
   float sum = 0.f;
+  if (how.formed) {
+    // subtracted first: a bias of the type's lowest value times log2 e would be an infinity
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - base, kLog2e, kOffset));
+  } else {
+    const float c = how.scale * kLog2e, shift = __builtin_fmaf(how.bias - base, kLog2e, kOffset);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, shift));
+  }
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[b][r] = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - shift, c, kOffset))
-                     : __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, shift));
-      sum += x[b][r];
-    }
+    for (int r = 0; r < 16; ++r) sum += x[b][r];
   run.sum += sum;
 }
 
+// What is multiplied instead of a scale of 0, which would make NaN of the -inf of hidden positions.
+constexpr float kAttnLeastScale = 1e-37f;
+
+// v where the bit of register r is set (word: shifted by 4 times the half), else `other`.
+__device__ __forceinline__ float attn_select(unsigned word, int r, float v, float other) {
+  const int all = (int)(word << (31 - (8 * (r / 4) + r % 4))) >> 31;
+  const int bits = (all & __builtin_bit_cast(int, v)) | (~all & __builtin_bit_cast(int, other));
+  return __builtin_bit_cast(float, bits);
+}
 // Scores that a column does not see become -inf.  word: bit per row of the block.
 __device__ __forceinline__ void attn_hide(f32x16& x, unsigned word, int half) {
   asm volatile("");                                      // keeps the caller's branch: two instructions per score are not for every tile
   const unsigned w = word >> (4 * half);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? x[r] : -__builtin_inff();
+  for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r], -__builtin_inff());
 }
 
 }  // namespace spdl

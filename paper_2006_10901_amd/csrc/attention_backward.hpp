@@ -13,24 +13,25 @@ namespace spdl {
 // so far then keep all bits of a term.
 struct AttnScale {
   float factor = 1.f, limit = 0.f;
-  // makes room for x and scales it; what has been summed is scaled along
-  template <int BLOCKS> __device__ __forceinline__ void fit(f32x16& x, f32x16 (&acc)[BLOCKS]) {
+  // makes room for x, which is taken times `by` already; what has been summed is scaled along.  Whether the factor has changed
+  template <int BLOCKS> __device__ __forceinline__ bool fit(f32x16& x, f32x16 (&acc)[BLOCKS], float by) {
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[r]));
-    if (__any(most > limit)) {
+    if (!__any(most > limit * by)) return false;
+    asm volatile("");
 #pragma unroll
-      for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-      // 2^11 for the largest here, room for sixteen times as much; powers within +-100, so that the factors at the end are normal
-      // numbers (a quotient that is not belongs to sums of less than 2^-126 of what comes)
-      const int e = min(max(11 - ilogbf(fminf(most, 1e30f)), -100), 100);
-      const float now = ldexpf(1.f, e), change = limit == 0.f ? 0.f : now / factor;
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    // 2^11 for the largest here, room for sixteen times as much; powers within +-100, so that the factors at the end are normal
+    // numbers (a quotient that is not belongs to sums of less than 2^-126 of what comes)
+    const int e = min(max(11 - ilogbf(fminf(most / by, 1e30f)), -100), 100);
+    const float now = ldexpf(1.f, e), change = limit == 0.f ? 0.f : now / factor;
 #pragma unroll
-      for (int b = 0; b < BLOCKS; ++b) acc[b] *= change;
-      factor = now;
-      limit = 32768.f / now;
-    }
-    x *= factor;
+    for (int b = 0; b < BLOCKS; ++b) acc[b] *= change;
+    x *= now / by;
+    factor = now;
+    limit = 32768.f / now;
+    return true;
   }
 };
 
@@ -38,7 +39,7 @@ struct AttnScale {
 __device__ __forceinline__ bool attn_far(int near, int span) { return near - 31 >= span || near + 31 <= -span; }
 
 // What a pass over a row's keys tells of the row: the sums of dS and of P over all of them and, for the gradient of the bias, over the
-// blocks that lie at its lower and at its upper end.  Added up in 64 bits: sums of thousands of terms that nearly cancel.
+// blocks that lie at its lower and at its upper end (half precision: of P only there).  Added up in 64 bits: sums of thousands of terms that nearly cancel.
 //
 // P comes from lse, which is rounded to 2^-24 of itself: an error of up to 5e-7 that all weights of a row share.  D is off by
 // what rounding O cost.  But P adds up to 1 over a row, and dS to 0, so that the sums tell both errors: weights are P / sum P, and D
@@ -52,14 +53,14 @@ template <typename T, bool BIAS> constexpr bool attn_row_sums() { return BIAS ||
 // What the other kernels take of a row: D, 1 / sum P (single precision) and the sums of dS at the ends.
 template <typename T, bool BIAS>
 __device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat, float delta, const AttnRowSums& s) {
-  const bool any = s.p > 0. && s.p < 1e30;                // not a row that sees nothing, nor one of Inf or NaN
-  const double weight = any ? 1. / s.p : 1., more = any ? s.ds * weight : 0.;
-  a.delta[flat] = (float)(delta + more);
+  // (half precision takes sum P as 1; a row of Inf or NaN keeps its D)
+  const bool usable = s.p > 0. && s.p < 1e30;
+  const double weight = sizeof(T) == 4 && usable ? 1. / s.p : 1., more = s.ds * weight;
+  a.delta[flat] = more == more ? (float)(delta + more) : delta;
   if constexpr (sizeof(T) == 4) a.weight[flat] = (float)weight;
   if constexpr (BIAS) {
-    const double f = sizeof(T) == 4 ? weight : 1.;
-    a.ends[2 * flat] = (float)(f * (s.low - more * s.low_p));
-    a.ends[2 * flat + 1] = (float)(f * (s.high - more * s.high_p));
+    a.ends[2 * flat] = (float)(weight * (s.low - more * s.low_p));
+    a.ends[2 * flat + 1] = (float)(weight * (s.high - more * s.high_p));
   }
 }
 template <typename T, bool BIAS>
@@ -79,23 +80,32 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttnArgs a) {
 template <typename T, int D, bool BIAS> struct AttnQueries {
   static constexpr int kTerms = attn_terms<T>();
   AttnOwn<D, kTerms> q, g;
-  float scale, c, shift, to_dp;
+  float scale, lse, to_dp;
   int64_t flat;
   __device__ __forceinline__ void load(const AttnArgs& a, const AttnPanelOf& at, const AttnFactors& f, int row, bool valid, int half) {
     flat = ((int64_t)at.batch * a.heads + at.head) * a.m + row;
     q.load(a.q16 + at.batch * a.q16s.batch + at.head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
     g.load(a.g16 + at.batch * a.g16s.batch + at.head * a.g16s.head, row * a.g16s.row, valid, a.width, half);
     if (a.scale < 0.f) q.negate();
-    scale = fabsf(a.scale) * (f.q * f.k);
-    c = BIAS ? kLog2e : scale * kLog2e;
+    scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
     to_dp = f.g * f.v;
-    float lse = valid ? a.lse[flat] : 0.f;
+    lse = valid ? a.lse[flat] : 0.f;
     if (lse == -__builtin_inff()) lse = __builtin_inff();  // a row that sees nothing has no weights
-    shift = BIAS ? lse : -lse * kLog2e;
   }
-  // x, y: Q K^T and dO V^T as the products leave them; x becomes P
-  __device__ __forceinline__ float weight(float x) const {
-    return BIAS ? __builtin_amdgcn_exp2f((x - shift) * c) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, shift));
+  // Products become weights, with one bias for all of them (AttnScores), or each with its own
+  __device__ __forceinline__ void weights(f32x16& x, float bias) const {
+    if (fabsf(bias) < kAttnLargeBias) {
+      const float c = scale * kLog2e, shift = (bias - lse) * kLog2e;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shift));
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f((__builtin_fmaf(x[r], scale, bias) - lse) * kLog2e);
+    }
+  }
+  __device__ __forceinline__ void weights(f32x16& x, const float* bias) const {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f((__builtin_fmaf(x[r], scale, bias[8 * (r / 4) + r % 4]) - lse) * kLog2e);
   }
 };
 
@@ -149,6 +159,7 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
     position = attn_position(a, batch);
   }
   AttnRowSums sums = {};
+  float to_ds = own.to_dp, delta_ds = delta, from_ds = 1.f;   // what makes dS, taken times the factor of ds_scale
 
   f32x16 acc[D / 32] = {};
   AttnScale ds_scale;
@@ -181,24 +192,34 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
       attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
       attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
       const bool far = BIAS && attn_far(near, a.span);
-      if (BIAS) {
-        if (far) attn_add_constant(x, own.scale, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
-        else attn_add_bias<1>(x, own.scale, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
-      }
+      if (!BIAS) own.weights(x, 0.f);
+      else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
+      else own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
-      float sum = 0.f, sum_p = 0.f;
+      const bool sum_weights = kTerms == 2 || far;
+      if (hide && sum_weights) {
+        asm volatile("");
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float p = own.weight(x[r]);
-        if (hide) p = attn_bit(w, r) ? p : 0.f;
-        x[r] = p * __builtin_fmaf(y[r], own.to_dp, -delta);
-        if (hide) x[r] = attn_bit(w, r) ? x[r] : 0.f;      // whatever stands where the row does not look
-        if (kSums) {
-          sum += x[r];
-          sum_p += p;
-        }
+        for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r], 0.f);
+      }
+      float sum = 0.f, sum_p = 0.f;
+      if (sum_weights) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum_p += x[r];
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= __builtin_fmaf(y[r], to_ds, -delta_ds);
+      if (hide) {                                          // whatever stands where the row does not look
+        asm volatile("");
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r], 0.f);
       }
       if (kSums) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += x[r];
+      }
+      if (kSums) {
+        sum *= from_ds;
         sums.ds += sum;
         sums.p += sum_p;
         if (BIAS && far) {
@@ -206,7 +227,7 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
           (near > 0 ? sums.high_p : sums.low_p) += sum_p;
         }
       }
-      ds_scale.fit(x, acc);
+      if (ds_scale.fit(x, acc, ds_scale.factor)) to_ds = own.to_dp * ds_scale.factor, delta_ds = delta * ds_scale.factor, from_ds = 1.f / ds_scale.factor;
       attn_product_t<D, kTerms>(acc, lds_k + b * 32 * Tile::kPitch, x, lane);
     }
   }
@@ -338,10 +359,10 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
       f32x16 x = {}, y = {};
       attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
       attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
-      attn_add_bias<1>(x, own.scale, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+      own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = attn_bit(w, r) ? own.weight(x[r]) * weight * __builtin_fmaf(y[r], own.to_dp, -delta) : 0.f;
+      for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r] * weight * __builtin_fmaf(y[r], own.to_dp, -delta), 0.f);
       attn_sum_diagonals(x, lds_blocks + wave * kAttnDiagonalBlock, sums, near, a.span, low, high, lane);
     }
   }
@@ -370,8 +391,9 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set: 64 times lse, D and what P is taken times
-  float* lds_bias = lds_stats + Tile::kSets * 3 * kAttnTile;
+  float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set, 64 times: lse (as an exponent of 2; with
+  // a bias lse itself, and the exponents with the bias's two ends), D, what P is taken times
+  float* lds_bias = lds_stats + Tile::kSets * 5 * kAttnTile;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
   const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
@@ -395,8 +417,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   vf.load(a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head, key * a.v16s.row, valid, a.width, half);
   if (a.scale < 0.f) kf.negate();
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
-  const float scale = fabsf(a.scale) * (f.q * f.k), to_dp = f.g * f.v;
-  const float c = BIAS ? kLog2e : scale * kLog2e;
+  const float scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale), to_dp = f.g * f.v, c = scale * kLog2e;
 
   const MaskLayout lay(a.m, a.k);
   const AttnSeenTiles seen_tiles(a.mask, lay.col_tiles, lay.ti, lay.tj, first_key);
@@ -430,29 +451,37 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
   };
   int64_t at = next(begin);
   int bias_head = -1;
+  float low = 0.f, high = 0.f;                            // the bias at its ends
   if (at < end) load(at);
   for (int set = 0; at < end; set ^= Tile::kSets - 1) {
     char* lds_q = lds_raw + set * Tile::kPair;
     char* lds_g = lds_q + kAttnTile * Tile::kPitch;
-    float* lds_lse = lds_stats + set * 3 * kAttnTile;
+    float* lds_lse = lds_stats + set * 5 * kAttnTile;
     float* lds_delta = lds_lse + kAttnTile;
     float* lds_weight = lds_delta + kAttnTile;
+    float* lds_ends = lds_weight + kAttnTile;
     if (Tile::kSets == 1) __syncthreads();
     stage_q.store(lds_q, tid);
     stage_g.store(lds_g, tid);
     const int h = (int)(at / tiles), row0 = (int)(at - (int64_t)h * tiles) * kAttnTile;
+    const uint64_t word = valid ? word_next : 0ull;
+    if (BIAS && h != bias_head) {
+      __syncthreads();                                    // the head before may still be at work
+      attn_fill_bias<T>(lds_bias, a, kv_head * a.group + h, tid, 256);
+      __syncthreads();
+      bias_head = h;
+      low = lds_bias[kAttnPad], high = lds_bias[2 * a.span + kAttnPad];
+    }
     if (tid < 64) {
       // rows that see nothing, and those behind the last, have no weights
       const float l = stat == -__builtin_inff() ? __builtin_inff() : stat;
       lds_lse[tid] = BIAS ? l : kOffset - l * kLog2e;
+      if (BIAS) {
+        lds_ends[tid] = __builtin_fmaf(low - l, kLog2e, kOffset);
+        lds_ends[64 + tid] = __builtin_fmaf(high - l, kLog2e, kOffset);
+      }
     } else if (tid < (kTerms == 2 ? 192 : 128)) {
       lds_lse[tid] = stat;
-    }
-    const uint64_t word = valid ? word_next : 0ull;
-    if (BIAS && h != bias_head) {
-      if (Tile::kSets == 2) __syncthreads();              // the head before may still be at work
-      attn_fill_bias<T>(lds_bias, a, kv_head * a.group + h, tid, 256);
-      bias_head = h;
     }
     __syncthreads();
     at = next(at + 1);
@@ -465,33 +494,40 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
       f32x16 x = {}, y = {};
       attn_product<D, kTerms>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
       attn_product<D, kTerms>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
-      if (BIAS) {
-        if (attn_far(near, a.span)) attn_add_constant(x, scale, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
-        else attn_add_bias<-1>(x, scale, lds_bias + kAttnPad + a.span + near + (lane & 31) - 4 * half);
-      }
-      const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
+      const bool far = BIAS && attn_far(near, a.span) && fabsf(near > 0 ? high : low) < kAttnLargeBias;
+      if (!BIAS || far) {
+        const float* shifts = (BIAS ? lds_ends + (near > 0 ? 64 : 0) : lds_lse) + b * 32 + half * 4;
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const f32x4 l = *reinterpret_cast<const f32x4*>(lds_lse + b * 32 + q4 * 8 + half * 4);
-        const f32x4 dl = *reinterpret_cast<const f32x4*>(lds_delta + b * 32 + q4 * 8 + half * 4);
-        f32x4 wt = {};
-        if constexpr (kTerms == 2) wt = *reinterpret_cast<const f32x4*>(lds_weight + b * 32 + q4 * 8 + half * 4);
+        for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shifts[8 * (r / 4) + r % 4]));
+      } else {
+        // the table's entries are read one by one, so that far positions of a large bias read its end
+        const int rel = near + (lane & 31) - 4 * half + a.span;
+        const float* l = lds_lse + b * 32 + half * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * q4 + e;
-          float p = BIAS ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[r] - l[e], c, kOffset)) : __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, l[e]));
-          if constexpr (kTerms == 2) p *= wt[e];
-          float s = p * __builtin_fmaf(y[r], to_dp, -dl[e]);
-          if (hide) {
-            p = attn_bit(w, r) ? p : 0.f;
-            s = attn_bit(w, r) ? s : 0.f;
-          }
-          x[r] = p;
-          y[r] = s;
+        for (int r = 0; r < 16; ++r) {
+          const float bias = lds_bias[kAttnPad + min(max(rel - (8 * (r / 4) + r % 4), 0), 2 * a.span)];
+          x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(x[r], scale, bias) - l[8 * (r / 4) + r % 4], kLog2e, kOffset));
         }
       }
+      if constexpr (kTerms == 2) {
+        const float* weights = lds_weight + b * 32 + half * 4;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] *= weights[8 * (r / 4) + r % 4];
+      }
+      if (hide) {
+        asm volatile("");
+        const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[r] = attn_select(w, r, x[r], 0.f);
+          y[r] = attn_select(w, r, y[r], 0.f);
+        }
+      }
+      const float* deltas = lds_delta + b * 32 + half * 4;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) y[r] = x[r] * __builtin_fmaf(y[r], to_dp, -deltas[8 * (r / 4) + r % 4]);
       attn_product_t<D, kTerms>(dv, lds_g + b * 32 * Tile::kPitch, x, lane);
-      ds_scale.fit(y, dk);
+      if (!ds_scale.fit(y, dk, 1.f)) y *= ds_scale.factor;
       attn_product_t<D, kTerms>(dk, lds_q + b * 32 * Tile::kPitch, y, lane);
     }
   }

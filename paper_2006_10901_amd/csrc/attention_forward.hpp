@@ -28,8 +28,7 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
   q.load(a.q16 + batch * a.q16s.batch + head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
   if (a.scale < 0.f) q.negate();                         // so that the largest score is the largest product
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
-  const float scale = fabsf(a.scale) * (f.q * f.k);
-  const float c = BIAS ? kLog2e : fmaxf(scale * kLog2e, 1e-37f);   // never 0: it meets the -inf of hidden positions
+  const float scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
 
   const MaskLayout lay(a.m, a.k);
   const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
@@ -65,14 +64,19 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
     f32x16 x[2] = {};
 #pragma unroll
     for (int b = 0; b < 2; ++b) attn_product<D, kTerms>(x[b], lds_k + b * 32 * Tile::kPitch, q, lane);
+    AttnScores how = {scale, false, 0.f};
     if (BIAS) {
       const int near = key0 - (position + wave_row);     // relative position of the tile's first key and the wave's first query
       if (near - 31 >= a.span || near + 63 <= -a.span) {
-        const float far = lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad];
+        how.bias = lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad];
+        how.formed = !(fabsf(how.bias) < kAttnLargeBias);
+        if (how.formed) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) attn_add_constant(x[b], scale, far);
+          for (int b = 0; b < 2; ++b) attn_add_constant(x[b], scale, how.bias);
+        }
       } else {
         const float* from = lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half;
+        how.formed = true;
 #pragma unroll
         for (int b = 0; b < 2; ++b) attn_add_bias<1>(x[b], scale, from + 32 * b);
       }
@@ -81,14 +85,14 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
       attn_hide(x[0], (unsigned)word, half);
       attn_hide(x[1], (unsigned)(word >> 32), half);
     }
-    attn_softmax_step<D, 2, BIAS>(x, run, acc, c);
+    attn_softmax_step<D, 2>(x, run, acc, how);
 #pragma unroll
     for (int b = 0; b < 2; ++b) attn_product_t<D, kTerms>(acc, lds_v + b * 32 * Tile::kPitch, x[b], lane);
   }
 
   const float total = attn_sum_halves(run.sum);
   const bool none = run.most == -__builtin_inff() && total == 0.f;
-  const float lse = none ? -__builtin_inff() : run.most * c * kLn2 + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
+  const float lse = none ? -__builtin_inff() : run.most + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
   const float inv = none ? 0.f : f.v / total;
   const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
   if (a.splits == 1) {
@@ -196,8 +200,7 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
 #pragma unroll
     for (int s = 0; s < Tile::kSteps; ++s) q[s] = -q[s];
   }
-  const float scale = fabsf(a.scale);
-  const float c = BIAS ? kLog2e : fmaxf(scale * kLog2e, 1e-37f);
+  const float scale = fmaxf(fabsf(a.scale), kAttnLeastScale);
   const MaskLayout lay(a.m, a.k);
   int position = 0, first = 0;
   float low = 0.f, high = 0.f;                           // the bias at its ends
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     f32x16 x[1] = {};
     token_product<D>(x[0], lds_k, q, lane);
     if (BIAS && (key0 - (first + a.m - 1) >= a.span || key0 + 31 - first <= -a.span)) {
-      attn_add_constant(x[0], scale, key0 > first ? high : low);
+      attn_add_constant(x[0], scale, key0 > first ? high : low);      // each lane's own head
     } else if (BIAS) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
       }
     }
     if (__any(word != ~0u)) attn_hide(x[0], word, half);
-    attn_softmax_step<D, 1, BIAS>(x, run, acc, c);
+    attn_softmax_step<D, 1>(x, run, acc, AttnScores{scale, BIAS, 0.f});
     token_product_t<D>(acc, lds_v, x[0], lane, T{});
   }
 
@@ -274,14 +277,14 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
       const float own = lds_stat[(w * 32 + r) * 2];
-      const float f = own == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((own - most) * c);
+      const float f = own == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((own - most) * kLog2e);
       const float s = lds_stat[(w * 32 + r) * 2 + 1], v = lds_acc[(w * 32 + r) * (D + 1) + col];
       // a wave that has seen only NaN has no maximum, and its sums count
       total += s == s ? s * f : s;
       value += v == v ? v * f : v;
     }
     const bool none = most == -__builtin_inff() && total == 0.f;
-    const float lse = none ? -__builtin_inff() : most * c * kLn2 + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
+    const float lse = none ? -__builtin_inff() : most + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
     const float result = none ? 0.f : value / total;
     const int64_t flat = ((int64_t)batch * a.heads + h) * a.m + i;
     if (a.splits == 1) {
