@@ -17,7 +17,8 @@ constexpr int kMostRows = 1 << 29;
 constexpr int kMostWidth = 128;
 
 struct Plan {
-  bool token;                          // the kernel for a few queries
+  bool token;                          // the kernel for a few queries, and how many rows its workgroups take
+  int token_rows;
   int forward_splits, dq_splits, dkv_splits, dbias_splits;
   int64_t forward_blocks, dq_blocks, dkv_blocks;      // without the splits
   int64_t rows, kv_rows, parts;        // parts: workgroups that leave sums of dS per head
@@ -44,7 +45,7 @@ inline int64_t take(int64_t& end, int64_t floats) {
 
 // How many workgroups a panel's work is split over: enough to give every compute unit `want` of them, of at least `least` steps each.
 inline int split_count(int64_t blocks, int64_t steps, int want, int least) {
-  if (blocks <= 0 || steps <= 0) return 1;
+  if (blocks <= 0 || steps <= 2 * least) return 1;
   const int64_t s = std::min<int64_t>(want * 256 / blocks, steps / least);
   return (int)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
@@ -56,19 +57,25 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   x.kv_rows = (int64_t)p.batch * p.kv_heads * p.k;
   x.width = kernel_width(p.d);
   x.token = p.m <= 16;
+  // Least steps per part: what a part saves has to pay for the kernel that joins (us, 1 / 2 / 4 steps: fp32 training step of 3 x 6 heads of 77 x 203 85 / 95 / 117,
+  // fp16 training step of 8 x 8 heads of 289 x 209 57 / 45 / 45, fp16 forward of 5 x 2 heads of 162 x 1242 16.0 / 14.6 / 14.2; single tokens, 4 / 8
+  // blocks of 32 keys: fp32 2 x 4 heads on 361 keys 18 / 26, fp16 7 x 14 rows on 3547 keys 23 / 19).
+  const bool f32 = elem_bytes == 4;
+  const int least_forward = f32 ? 1 : 4, least_backward = f32 ? 1 : 2;
   if (x.token) {
-    x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, 32);
-    x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 4, 8);
+    x.token_rows = !f32 ? 32 : group * p.m <= 4 ? 4 : group * p.m <= 8 ? 8 : 16;
+    x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, x.token_rows);
+    x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 2, f32 ? 4 : 8);
   } else {
     x.forward_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), 2, 4);
+    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), 2, least_forward);
   }
   x.dq_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, 4);
+  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, least_backward);
   x.dkv_blocks = (int64_t)p.batch * p.kv_heads * up(p.k, kAttnPanel);
-  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, 4);
+  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, least_backward);
   // tiles near the diagonal that a panel meets
-  x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 2);
+  x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 1);
   x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dbias_splits;
   x.most_parts = (int)std::min<int64_t>(64, std::max<int64_t>(1, up(std::max<int64_t>(group * p.m, p.k), 64)));
 
@@ -190,8 +197,8 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
   o.batch = a.batch, o.kv_heads = a.kv_heads, o.d = a.d, o.k = a.k, o.parts = x.most_parts, o.lengths = a.lengths;
   o.most = reinterpret_cast<float*>(w + x.most), o.factors = reinterpret_cast<float*>(w + x.factors);
   const int64_t each = (int64_t)a.batch * a.kv_heads * o.count;
-  // up to 2^13 numbers of a head every wave looks for the largest itself
-  if (std::max<int64_t>((int64_t)a.group * a.m, a.k) * a.d <= 8192) {
+  // of few numbers the workgroups that make the terms find the largest themselves, which saves a launch
+  if (std::max<int64_t>((int64_t)a.group * a.m, a.k) * a.d <= 32768) {
     o.most = nullptr;
   } else if (sizeof(T) == 4) {
     attention_largest_kernel<<<dim3((unsigned)(each * o.parts)), dim3(256), 0, stream>>>(o);
@@ -205,12 +212,22 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
 template <typename T, int D, bool BIAS>
 bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   if (x.token) {
-    const int lds = kAttnWaves * 2 * 32 * TokenTile<T, D>::kPitch + (BIAS ? std::min(a.group, 32) * a.buckets * 4 + (2 * a.span + 1) * 4 : 0);
-    return launch(attention_token_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream);
+    const int bias = BIAS ? std::min(a.group, x.token_rows) * a.buckets * 4 + (2 * a.span + 1) * 4 : 0;
+    const int64_t blocks = x.forward_blocks * a.splits;
+    if constexpr (sizeof(T) == 2) {
+      // K and V of four waves, later their parts
+      const int lds = std::max(kAttnWaves * 2 * 32 * AttnTile<D, 1>::kPitch + bias, kAttnWaves * 32 * (D + 1 + 2) * 4);
+      return launch(attention_token_kernel<D, BIAS>, blocks, lds, a, stream);
+    } else {
+      const int lds = std::max(bias, 4 * kAttnWaves * x.token_rows * ((D + 63) / 64 * 64 + 4 + 2) * 4);
+      return x.token_rows == 4   ? launch(attention_token_f32_kernel<D, 4, BIAS>, blocks, lds, a, stream)
+             : x.token_rows == 8 ? launch(attention_token_f32_kernel<D, 8, BIAS>, blocks, lds, a, stream)
+                                 : launch(attention_token_f32_kernel<D, 16, BIAS>, blocks, lds, a, stream);
+    }
   }
   if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
   using Tile = AttnTile<D, attn_terms<T>()>;
-  const int lds = Tile::kSets * Tile::kPair + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
+  const int lds = Tile::kSets * kAttnTile * (Tile::kPitch + Tile::kPitchT) + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
   return launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream);
 }
 
@@ -292,7 +309,7 @@ int attention(const spdl_attention_problem* p, const void* Q, const void* K, con
   (void)hipGetLastError();
   if (!(table ? dispatch_forward<T, true>(x, a, w, s) : dispatch_forward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (a.splits > 1) {
-    attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 16)), dim3(256), 0, s>>>(a);
+    attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 4)), dim3(256), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   }
   return SPDL_OK;

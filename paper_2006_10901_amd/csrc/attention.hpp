@@ -106,11 +106,11 @@ __device__ __forceinline__ typename AttnPiece<T>::Type attn_load_piece(const T* 
   }
   return v;
 }
-// The same for rows of whole pieces, without a branch: pieces that are not wanted read one that is there.
+// The same for rows of whole pieces, without a branch and without looking at what comes (that would wait for it): pieces behind the row's
+// end are its last one again.  They meet zeros of the other operand, or columns that are not stored.
 template <typename T>
-__device__ __forceinline__ typename AttnPiece<T>::Type attn_load_whole_piece(const T* row, int c0, int d, bool wanted) {
-  const typename AttnPiece<T>::Type v = *reinterpret_cast<const typename AttnPiece<T>::Any*>(row + min(c0, d - 16 / (int)sizeof(T)));
-  return wanted && c0 < d ? v : typename AttnPiece<T>::Type{};
+__device__ __forceinline__ typename AttnPiece<T>::Type attn_load_whole_piece(const T* row, int c0, int d) {
+  return *reinterpret_cast<const typename AttnPiece<T>::Any*>(row + min(c0, d - 16 / (int)sizeof(T)));
 }
 
 // A tile on its way from memory to LDS, requested a tile ahead into registers, then written: ROWS rows of BYTES bytes, PITCH apart.
@@ -119,7 +119,8 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
   static constexpr int kElements = 16 / (int)sizeof(T), kPieces = BYTES / 16, kCount = ROWS * kPieces / THREADS;
   static_assert(ROWS * kPieces % THREADS == 0, "whole pieces per thread");
   Piece v[kCount];
-  // rows [0, rows) of `base`, `stride` elements apart, of d elements, a multiple of a piece's; zeros behind them (rows >= 1)
+  // rows [0, rows) of `base`, `stride` elements apart, of d elements, a multiple of a piece's (rows >= 1); behind them the last one again,
+  // whose weights are 0 there
   __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d, int tid) {
     if (rows >= ROWS && d * (int)sizeof(T) == BYTES) {
 #pragma unroll
@@ -131,7 +132,7 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
 #pragma unroll
       for (int i = 0; i < kCount; ++i) {
         const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
-        v[i] = attn_load_whole_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d, row < rows);
+        v[i] = attn_load_whole_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d);
       }
     }
   }
@@ -141,8 +142,7 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
       const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
-      v[i] = Piece{};
-      if (row < rows) v[i] = attn_load_piece<T>(base + row * stride, c * kElements, d);
+      v[i] = attn_load_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d);
     }
   }
   __device__ __forceinline__ void store(char* lds, int tid) const {
@@ -161,7 +161,10 @@ template <int D, int TERMS> struct AttnTile {
   // Two tiles (K and V, or Q and dO) at a time, in two sets where two workgroups then fit a compute unit: one is written while the other
   // is read, and the workgroup meets once per tile.
   static constexpr int kPair = 2 * kAttnTile * kPitch, kSets = 2 * kPair <= 72 * 1024 ? 2 : 1;
-  template <int ROWS, int THREADS> using Stage = AttnStage<_Float16, ROWS, kBytes, kPitch, THREADS>;
+  // A tile that is only read by the reads that transpose (V in the forward pass), 64 bytes of four rows at a time: an odd multiple of
+  // 64 bytes puts those into all 64 banks, where 16 bytes past a multiple of 256 lets four rows meet in one.
+  static constexpr int kPitchT = ((kBytes + 63) / 64 | 1) * 64;
+  template <int ROWS, int THREADS, int PITCH = kPitch> using Stage = AttnStage<_Float16, ROWS, kBytes, PITCH, THREADS>;
 };
 // The own operand: pieces of row `lane % 32`, the half of the lane.
 template <int D, int TERMS> struct AttnOwn {
@@ -172,7 +175,11 @@ template <int D, int TERMS> struct AttnOwn {
 #pragma unroll
     for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s) v[t][s] = attn_load_whole_piece<_Float16>(row, t * D + (2 * s + half) * 8, d, valid);
+      for (int s = 0; s < D / 16; ++s) {
+        const int c = t * D + (2 * s + half) * 8;
+        const f16x8 piece = attn_load_whole_piece<_Float16>(row, c, d);
+        v[t][s] = valid && c < d ? piece : f16x8{};
+      }
   }
   __device__ __forceinline__ void negate() {
 #pragma unroll
@@ -211,16 +218,15 @@ __device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const A
 }
 
 // acc (D x 32, blocks of 32) += (32 rows of the tile)^T X
-template <int D, int TERMS>
+template <int D, int TERMS, int PITCH = AttnTile<D, TERMS>::kPitch>
 __device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane) {
   typedef __attribute__((address_space(3))) s16x4* LdsPtr;
   typedef short s16x8 __attribute__((ext_vector_type(8)));
-  constexpr int kPitch = AttnTile<D, TERMS>::kPitch;
   const int i = lane & 15;
-  const char* at = lds + (4 * (lane >> 5) + (i >> 2)) * kPitch + (((lane >> 4) & 1) * 16 + (i & 3) * 4) * 2;
+  const char* at = lds + (4 * (lane >> 5) + (i >> 2)) * PITCH + (((lane >> 4) & 1) * 16 + (i & 3) * 4) * 2;
   auto left = [&](int s, int offset) {
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s) * kPitch + offset));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s + 8) * kPitch + offset));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s) * PITCH + offset));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + (16 * s + 8) * PITCH + offset));
     return __builtin_bit_cast(f16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
 #pragma unroll
@@ -417,10 +423,11 @@ struct AttnRunning { float most = -__builtin_inff(), sum = 0.f; };
 constexpr float kAttnLargeBias = 1e6f;
 struct AttnScores { float scale; bool formed; float bias; };
 
-// x: NB blocks of products (AttnScores::formed: of scores); turns them into weights relative to the running maximum and scales what has
-// been summed before.
+// x: NB blocks of products (AttnScores::formed: of scores).  Brings the running maximum up to date, scales what has been summed before,
+// and says how a product becomes a weight relative to that maximum: 2^(c x + shift).
+struct AttnExponent { float c, shift; };
 template <int D, int NB>
-__device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& run, f32x16 (&acc)[D / 32], const AttnScores& how) {
+__device__ __forceinline__ AttnExponent attn_softmax_step(f32x16 (&x)[NB], AttnRunning& run, f32x16 (&acc)[D / 32], const AttnScores& how) {
   float most = -__builtin_inff();
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -439,24 +446,22 @@ __device__ __forceinline__ void attn_softmax_step(f32x16 (&x)[NB], AttnRunning& 
     run.most = now;
   }
   const float base = run.most == -__builtin_inff() ? 0.f : run.most;
-  float sum = 0.f;
-  if (how.formed) {
-    // subtracted first: a bias of the type's lowest value times log2 e would be an infinity
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r] - base, kLog2e, kOffset));
-  } else {
-    const float c = how.scale * kLog2e, shift = __builtin_fmaf(how.bias - base, kLog2e, kOffset);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], c, shift));
-  }
+  if (!how.formed) return {how.scale * kLog2e, __builtin_fmaf(how.bias - base, kLog2e, kOffset)};
+  // subtracted first: a bias of the type's lowest value times log2 e would be an infinity
+  asm volatile("");
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sum += x[b][r];
+    for (int r = 0; r < 16; ++r) x[b][r] -= base;
+  return {kLog2e, kOffset};
+}
+__device__ __forceinline__ void attn_weights(f32x16& x, AttnRunning& run, const AttnExponent& to) {
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], to.c, to.shift));
+    sum += x[r];
+  }
   run.sum += sum;
 }
 

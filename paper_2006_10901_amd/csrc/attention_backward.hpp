@@ -110,8 +110,11 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
 };
 
 // dQ, by panels of 128 queries, and D = dO . O.
+//
+// Two workgroups to a compute unit, with 256 registers a thread, where that spills few of them (us, one -> two: fp16, 128 columns, 2 x 8 heads of
+// 2048 x 2048 99 -> 74; fp32, 64 columns, 8 heads of 4096 x 4096 270 -> 207; but fp32 96 and 128 columns 93 -> 149 and 121 -> 237).
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void attention_dq_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   constexpr bool kSums = attn_row_sums<T, BIAS>();
   using Tile = AttnTile<D, kTerms>;
@@ -191,6 +194,7 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
       f32x16 x = {}, y = {};
       attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
       attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+      __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
       const bool far = BIAS && attn_far(near, a.span);
       if (!BIAS) own.weights(x, 0.f);
       else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
@@ -229,6 +233,7 @@ __global__ __launch_bounds__(256) void attention_dq_kernel(const AttnArgs a) {
       }
       if (ds_scale.fit(x, acc, ds_scale.factor)) to_ds = own.to_dp * ds_scale.factor, delta_ds = delta * ds_scale.factor, from_ds = 1.f / ds_scale.factor;
       attn_product_t<D, kTerms>(acc, lds_k + b * 32 * Tile::kPitch, x, lane);
+      __builtin_amdgcn_s_setprio(0);
     }
   }
 
@@ -386,8 +391,9 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
 }
 
 // dK and dV, by panels of 128 keys: a wave has 32 of them, tiles of 64 queries, of every head that shares the keys, are shared by the waves.
+// Two workgroups to a compute unit as for dQ (fp32, 64 columns 369 -> 292 us, fp16 96 106 -> 98), but not at 128 columns (fp16 143 -> 235).
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1) void attention_dkv_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
@@ -494,6 +500,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
       f32x16 x = {}, y = {};
       attn_product<D, kTerms>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
       attn_product<D, kTerms>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
+      __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
       const bool far = BIAS && attn_far(near, a.span) && fabsf(near > 0 ? high : low) < kAttnLargeBias;
       if (!BIAS || far) {
         const float* shifts = (BIAS ? lds_ends + (near > 0 ? 64 : 0) : lds_lse) + b * 32 + half * 4;
@@ -529,6 +536,7 @@ __global__ __launch_bounds__(256) void attention_dkv_kernel(const AttnArgs a) {
       attn_product_t<D, kTerms>(dv, lds_g + b * 32 * Tile::kPitch, x, lane);
       if (!ds_scale.fit(y, dk, 1.f)) y *= ds_scale.factor;
       attn_product_t<D, kTerms>(dk, lds_q + b * 32 * Tile::kPitch, y, lane);
+      __builtin_amdgcn_s_setprio(0);
     }
   }
 

@@ -7,11 +7,12 @@ namespace spdl {
 
 // Panels of 128 queries: a wave has 32 of them, tiles of 64 keys are shared by the four waves.
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void attention_forward_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
+  constexpr int kPair = kAttnTile * (Tile::kPitch + Tile::kPitchT);
+  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * kPair);
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
   const AttnPanelOf at(a, a.m);
@@ -40,7 +41,8 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
 
   f32x16 acc[D / 32] = {};
   AttnRunning run;
-  typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  typename Tile::template Stage<kAttnTile, 256> stage_k;
+  typename Tile::template Stage<kAttnTile, 256, Tile::kPitchT> stage_v;
   uint64_t word_next = 0;
   auto load = [&](int t) {
     word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
@@ -50,7 +52,7 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
   int t = tiles.next(begin, end);
   if (t < end) load(t);
   for (int set = 0; t < end; set ^= Tile::kSets - 1) {
-    char* lds_k = lds_raw + set * Tile::kPair;
+    char* lds_k = lds_raw + set * kPair;
     char* lds_v = lds_k + kAttnTile * Tile::kPitch;
     if (Tile::kSets == 1) __syncthreads();
     stage_k.store(lds_k, tid);
@@ -85,9 +87,16 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
       attn_hide(x[0], (unsigned)word, half);
       attn_hide(x[1], (unsigned)(word >> 32), half);
     }
-    attn_softmax_step<D, 2>(x, run, acc, how);
+    const AttnExponent to = attn_softmax_step<D, 2>(x, run, acc, how);
+    // a wave that has weights to form and multiply goes before one that only multiplies: the vector and the matrix instructions of two
+    // waves then meet more often (cross attention of 4096 x 8192, heads of 128: 342 -> 317 us)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) attn_product_t<D, kTerms>(acc, lds_v + b * 32 * Tile::kPitch, x[b], lane);
+    for (int b = 0; b < 2; ++b) {
+      attn_weights(x[b], run, to);
+      attn_product_t<D, kTerms, Tile::kPitchT>(acc, lds_v + b * 32 * Tile::kPitchT, x[b], lane);
+    }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   const float total = attn_sum_halves(run.sum);
@@ -106,52 +115,70 @@ __global__ __launch_bounds__(256) void attention_forward_kernel(const AttnArgs a
   }
 }
 
-// Single tokens are bound by reading K and V: in single precision they are multiplied as they are, on the fp32 instructions.
-template <typename T, int D> struct TokenTile {
-  static constexpr int kBytes = D * (int)sizeof(T), kPitch = kBytes + 16, kSteps = kBytes / 32, kPiece = 16 / sizeof(T);
+// Rows of a head of K and V in the kernels for a few queries: those of all query heads that share it, m of each, ROWS to a workgroup.
+template <int ROWS> struct TokenPanel {
+  int rows, split, panel, batch, kv_head;
+  __device__ __forceinline__ TokenPanel(const AttnArgs& a) {
+    rows = a.group * a.m;
+    const int panels = (rows + ROWS - 1) / ROWS;
+    int work = blockIdx.x;
+    split = work % a.splits;
+    work /= a.splits;
+    panel = work % panels;
+    work /= panels;
+    kv_head = work % a.kv_heads;
+    batch = work / a.kv_heads;
+  }
 };
-template <typename T, int D> using TokenOwn = typename AttnPiece<T>::Type[TokenTile<T, D>::kSteps];
 
-template <int D>
-__device__ __forceinline__ void token_product(f32x16& x, const char* lds, const TokenOwn<_Float16, D>& own, int lane) {
-  const char* row = lds + (lane & 31) * TokenTile<_Float16, D>::kPitch + (lane >> 5) * 16;
+// Joins PARTS parts of the keys that lie in LDS, each with its own maximum and sum: each is scaled to the common maximum, then they are
+// added up in their order.  offset: the power of two that weights were taken times.
+template <typename T, int ROWS, int PARTS, int PITCH>
+__device__ __forceinline__ void token_finish(const AttnArgs& a, const TokenPanel<ROWS>& at, const float* parts, const float* stats, float offset, int tid) {
+  const int64_t all = (int64_t)a.batch * a.heads * a.m;
+  for (int x = tid; x < ROWS * a.d; x += 256) {
+    const int r = x / a.d, col = x - r * a.d, p = at.panel * ROWS + r;
+    if (p >= at.rows) break;
+    const int g = p / a.m, i = p - g * a.m, h = at.kv_head * a.group + g;
+    float most = -__builtin_inff();
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8*>(row + s * 32), own[s], x, 0, 0, 0);
-}
-template <int D>
-__device__ __forceinline__ void token_product(f32x16& x, const char* lds, const TokenOwn<float, D>& own, int lane) {
-  const char* row = lds + (lane & 31) * TokenTile<float, D>::kPitch + (lane >> 5) * 16;
+    for (int w = 0; w < PARTS; ++w) most = fmaxf(most, stats[(w * ROWS + r) * 2]);
+    float total = 0.f, value = 0.f;
 #pragma unroll
-  for (int s = 0; s < D / 8; ++s) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(row + s * 32);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], own[s][e], x, 0, 0, 0);
+    for (int w = 0; w < PARTS; ++w) {
+      const float own = stats[(w * ROWS + r) * 2];
+      const float f = own == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((own - most) * kLog2e);
+      const float s = stats[(w * ROWS + r) * 2 + 1], v = parts[(w * ROWS + r) * PITCH + col];
+      // a part that has seen only NaN has no maximum, and its sums count
+      total += s == s ? s * f : s;
+      value += v == v ? v * f : v;
+    }
+    const bool none = most == -__builtin_inff() && total == 0.f;
+    const float lse = none ? -__builtin_inff() : most + (__builtin_amdgcn_logf(total) - offset) * kLn2;
+    const float result = none ? 0.f : value / total;
+    const int64_t flat = ((int64_t)at.batch * a.heads + h) * a.m + i;
+    if (a.splits == 1) {
+      (static_cast<T*>(a.O) + at.batch * a.o.batch + h * a.o.head + (int64_t)i * a.o.row)[col] = (T)result;
+      if (col == 0 && a.lse) a.lse[flat] = lse;
+    } else {
+      a.part[(at.split * all + flat) * a.d + col] = result;
+      if (col == 0) a.part_lse[at.split * all + flat] = lse;
+    }
   }
 }
-template <int D>
-__device__ __forceinline__ void token_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, _Float16) {
-  attn_product_t<D, 1>(acc, lds, x, lane);
-}
-template <int D>
-__device__ __forceinline__ void token_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane, float) {
-  constexpr int kPitch = TokenTile<float, D>::kPitch;
-  const char* at = lds + 4 * (lane >> 5) * kPitch + (lane & 31) * 4;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-#pragma unroll
-    for (int blk = 0; blk < D / 32; ++blk)
-      acc[blk] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + (8 * (r / 4) + r % 4) * kPitch + blk * 128), x[r],
-                                                      acc[blk], 0, 0, 0);
-  }
+
+// The number N lanes on within 16.
+template <int N> __device__ __forceinline__ float token_rotate(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
 }
 
 // A few queries: the rows of a head of K and V are those of all query heads that share it, m of each, 32 to a workgroup.  K and V are
 // read once per 32 rows.  The four waves take blocks of 32 keys in turn, each with its own statistics, and no wave waits for another
 // before the end.
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) {
-  using Tile = TokenTile<T, D>;
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs a) {
+  using T = _Float16;
+  using Tile = AttnTile<D, 1>;
   constexpr int kBlock = 32 * Tile::kPitch;              // 32 keys or values of a wave
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
@@ -161,13 +188,8 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
   float* lds_table = reinterpret_cast<float*>(lds_raw + kAttnWaves * 2 * kBlock);
   int* lds_bucket = reinterpret_cast<int*>(lds_table + min(a.group, 32) * a.buckets);
 
-  const int rows = a.group * a.m, panels = (rows + 31) / 32;
-  int work = blockIdx.x;
-  const int split = work % a.splits;
-  work /= a.splits;
-  const int panel = work % panels;
-  work /= panels;
-  const int kv_head = work % a.kv_heads, batch = work / a.kv_heads;
+  const TokenPanel<32> at(a);
+  const int rows = at.rows, split = at.split, panel = at.panel, batch = at.batch, kv_head = at.kv_head;
 
   const int seen = a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k;
   const int blocks_all = (a.k + 31) / 32;
@@ -190,16 +212,13 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     stage_k.load_any(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
     stage_v.load_any(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
   }
-  TokenOwn<T, D> q;
+  AttnOwn<D, 1> q;
 #pragma unroll
-  for (int s = 0; s < Tile::kSteps; ++s) {
-    q[s] = typename AttnPiece<T>::Type{};
-    if (valid) q[s] = attn_load_piece<T>(Q, (2 * s + half) * Tile::kPiece, a.d);
+  for (int s = 0; s < D / 16; ++s) {
+    q.v[0][s] = f16x8{};
+    if (valid) q.v[0][s] = attn_load_piece<T>(Q, (2 * s + half) * 8, a.d);
   }
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int s = 0; s < Tile::kSteps; ++s) q[s] = -q[s];
-  }
+  if (a.scale < 0.f) q.negate();
   const float scale = fmaxf(fabsf(a.scale), kAttnLeastScale);
   const MaskLayout lay(a.m, a.k);
   int position = 0, first = 0;
@@ -235,7 +254,7 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     word &= attn_low_bits(seen - key0);
     if (!__any(word != 0)) continue;
     f32x16 x[1] = {};
-    token_product<D>(x[0], lds_k, q, lane);
+    attn_product<D, 1>(x[0], lds_k, q, lane);
     if (BIAS && (key0 - (first + a.m - 1) >= a.span || key0 + 31 - first <= -a.span)) {
       attn_add_constant(x[0], scale, key0 > first ? high : low);      // each lane's own head
     } else if (BIAS) {
@@ -246,14 +265,14 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
       }
     }
     if (__any(word != ~0u)) attn_hide(x[0], word, half);
-    attn_softmax_step<D, 1>(x, run, acc, AttnScores{scale, BIAS, 0.f});
-    token_product_t<D>(acc, lds_v, x[0], lane, T{});
+    attn_weights(x[0], run, attn_softmax_step<D, 1>(x, run, acc, AttnScores{scale, BIAS, 0.f}));
+    attn_product_t<D, 1>(acc, lds_v, x[0], lane);
   }
 
-  // the four waves' parts: each scaled to the common maximum, then added up in the waves' order
+  // the four waves' parts, in LDS: [4][32][D + 1] sums, [4][32][2] statistics
   __syncthreads();
-  float* lds_acc = reinterpret_cast<float*>(lds_raw);                     // [4][32][D + 1]
-  float* lds_stat = lds_acc + kAttnWaves * 32 * (D + 1);                  // [4][32][2]
+  float* lds_acc = reinterpret_cast<float*>(lds_raw);
+  float* lds_stat = lds_acc + kAttnWaves * 32 * (D + 1);
   const float sum = attn_sum_halves(run.sum);
 #pragma unroll
   for (int blk = 0; blk < D / 32; ++blk)
@@ -265,77 +284,226 @@ __global__ __launch_bounds__(256) void attention_token_kernel(const AttnArgs a) 
     lds_stat[(wave * 32 + lane) * 2 + 1] = sum;
   }
   __syncthreads();
-  const int64_t all = (int64_t)a.batch * a.heads * a.m;
-  for (int at = tid; at < 32 * a.d; at += 256) {
-    const int r = at / a.d, col = at - r * a.d, p = panel * 32 + r;
-    if (p >= rows) break;
-    const int g = p / a.m, i = p - g * a.m, h = kv_head * a.group + g;
-    float most = -__builtin_inff();
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) most = fmaxf(most, lds_stat[(w * 32 + r) * 2]);
-    float total = 0.f, value = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-      const float own = lds_stat[(w * 32 + r) * 2];
-      const float f = own == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((own - most) * kLog2e);
-      const float s = lds_stat[(w * 32 + r) * 2 + 1], v = lds_acc[(w * 32 + r) * (D + 1) + col];
-      // a wave that has seen only NaN has no maximum, and its sums count
-      total += s == s ? s * f : s;
-      value += v == v ? v * f : v;
-    }
-    const bool none = most == -__builtin_inff() && total == 0.f;
-    const float lse = none ? -__builtin_inff() : most + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
-    const float result = none ? 0.f : value / total;
-    const int64_t flat = ((int64_t)batch * a.heads + h) * a.m + i;
-    if (a.splits == 1) {
-      (static_cast<T*>(a.O) + batch * a.o.batch + h * a.o.head + (int64_t)i * a.o.row)[col] = (T)result;
-      if (col == 0 && a.lse) a.lse[flat] = lse;
-    } else {
-      a.part[(split * all + flat) * a.d + col] = result;
-      if (col == 0) a.part_lse[split * all + flat] = lse;
-    }
-  }
+  token_finish<T, 32, kAttnWaves, D + 1>(a, at, lds_acc, lds_stat, kOffset, tid);
 }
 
-// Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s, in the parts' order.  16 lanes per row, four neighbouring
-// elements each.
+// The same in single precision, whose products are made as they are, by instructions that multiply 4 x 1 by 1 x 4 numbers in each
+// of sixteen blocks (fp32 instructions of 32 x 32 would do eight times the work for up to four rows, and took 54 us where this takes MEASURED).
+//
+// Lane l is row i = l % 4 of block l / 4 of the left operand and column i of that block of the right one.  Blocks split 16 keys into
+// four sets g = l / 16 of four, and columns into quarters u = l / 4 % 4:
+//   scores: lane l has 16 bytes of key 4 g + i, columns 16 t + 4 u .. + 3, and of row i of Q the same columns.  Register r of the result,
+//     added up over the quarters (lanes l, l + 4, l + 8, l + 12), is the score of key 4 g + r and row i;
+//   values: that register, as a weight, is the right operand for key 4 g + r; the left one is element e of lane l's 16 bytes of V, columns
+//     64 t + 16 u + 4 i + e.  Register j of the result is column 64 t + 16 u + 4 j + e and row i, of set g.
+// No number of K or V passes through LDS, all loads are of 64 bytes and more at a time, and each set has statistics of its own.
+// ROWS: rows of the workgroup, four to each group of registers.
+template <int D, int ROWS, bool BIAS>
+__global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_token_f32_kernel(const AttnArgs a) {
+  using T = float;
+  constexpr int kGroups = ROWS / 4, kScoreSteps = D / 16, kValueSteps = (D + 63) / 64, kSets = kAttnWaves * 4;
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i = lane & 3, g = lane >> 4, u = lane >> 2 & 3;
+  const TokenPanel<ROWS> at(a);
+  const int batch = at.batch, kv_head = at.kv_head;
+  const int seen = attn_seen(a, batch);
+  const int all = (a.k + 15) / 16, begin = (int)((int64_t)all * at.split / a.splits),
+            end = min((int)((int64_t)all * (at.split + 1) / a.splits), (seen + 15) / 16);
+  const T* K = static_cast<const T*>(a.K) + batch * a.kk.batch + kv_head * a.kk.head;
+  const T* V = static_cast<const T*>(a.V) + batch * a.v.batch + kv_head * a.v.head;
+  const bool whole = a.d % 4 == 0;
+
+  f32x4 kf[kScoreSteps], vf[4][kValueSteps];
+  // (rows behind the sequence's last are the last one again, with weights of 0)
+  auto load_keys = [&](int t) {
+    const T* row = K + (int64_t)min(t * 16 + 4 * g + i, seen - 1) * a.kk.row;
+    if (whole) {
+#pragma unroll
+      for (int s = 0; s < kScoreSteps; ++s) kf[s] = attn_load_whole_piece<T>(row, 16 * s + 4 * u, a.d);
+    } else {
+#pragma unroll
+      for (int s = 0; s < kScoreSteps; ++s) kf[s] = attn_load_piece<T>(row, 16 * s + 4 * u, a.d);
+    }
+  };
+  auto load_values = [&](int t) {
+    if (whole) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int s = 0; s < kValueSteps; ++s)
+          vf[r][s] = attn_load_whole_piece<T>(V + (int64_t)min(t * 16 + 4 * g + r, seen - 1) * a.v.row, 64 * s + 16 * u + 4 * i, a.d);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int s = 0; s < kValueSteps; ++s)
+          vf[r][s] = attn_load_piece<T>(V + (int64_t)min(t * 16 + 4 * g + r, seen - 1) * a.v.row, 64 * s + 16 * u + 4 * i, a.d);
+    }
+  };
+  int t = begin + wave;
+  if (t < end) {
+    load_keys(t);
+    load_values(t);
+  }
+
+  f32x4 q[kGroups][kScoreSteps];
+  int row[kGroups];
+  const float* table[kGroups];
+  float low[kGroups], high[kGroups];
+  const float scale = a.scale;
+  float* lds_table = reinterpret_cast<float*>(lds_raw);                   // the tables of the panel's heads, then the buckets
+  int* lds_bucket = reinterpret_cast<int*>(lds_table + min(a.group, ROWS) * a.buckets);
+  const int head0 = at.panel * ROWS / a.m;               // of the group, the first one in this panel
+  int first = 0;
+  if (BIAS) {
+    const int heads = min(a.group - head0, ROWS);
+    const T* from = static_cast<const T*>(a.table) + (int64_t)(kv_head * a.group + head0) * a.buckets;
+    for (int x = tid; x < heads * a.buckets; x += 256) lds_table[x] = from[x];
+    for (int x = tid; x < 2 * a.span + 1; x += 256) lds_bucket[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
+    first = attn_position(a, batch);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int c = 0; c < kGroups; ++c) {
+    const int packed = at.panel * ROWS + 4 * c + i;
+    const bool valid = packed < at.rows;
+    const int of_group = valid ? packed / a.m : head0;
+    row[c] = valid ? packed - of_group * a.m : 0;
+    const T* Q = static_cast<const T*>(a.Q) + batch * a.q.batch + (kv_head * a.group + of_group) * a.q.head + (int64_t)row[c] * a.q.row;
+#pragma unroll
+    for (int s = 0; s < kScoreSteps; ++s) q[c][s] = valid ? attn_load_piece<T>(Q, 16 * s + 4 * u, a.d) : f32x4{};
+    if (BIAS) {
+      table[c] = lds_table + (of_group - head0) * a.buckets;
+      low[c] = table[c][lds_bucket[0]], high[c] = table[c][lds_bucket[2 * a.span]];
+    }
+  }
+  const MaskLayout lay(a.m, a.k);
+
+  f32x4 acc[kGroups][kValueSteps][4] = {};
+  float most[kGroups], sum[kGroups];
+#pragma unroll
+  for (int c = 0; c < kGroups; ++c) most[c] = -__builtin_inff(), sum[c] = 0.f;
+  for (; t < end; t += kAttnWaves) {
+    const int key0 = t * 16;
+    f32x4 x[kGroups] = {};
+#pragma unroll
+    for (int s = 0; s < kScoreSteps; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < kGroups; ++c) x[c] = __builtin_amdgcn_mfma_f32_4x4x1f32(kf[s][e], q[c][s][e], x[c], 0, 0, 0);
+    if (t + kAttnWaves < end) load_keys(t + kAttnWaves);
+#pragma unroll
+    for (int c = 0; c < kGroups; ++c) {
+      unsigned word = attn_low_bits(seen - key0);
+      if (a.mask) word &= (unsigned)(a.mask[lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 + row[c]] >> (key0 & 63));
+      word >>= 4 * g;
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float s = x[c][r];
+        s += token_rotate<4>(s);
+        s += token_rotate<8>(s);
+        s *= scale;
+        if (BIAS) {
+          const int rel = key0 + 4 * g + r - first - row[c];
+          // far from the diagonal, where most keys are, the bias is one of two
+          s += rel <= -a.span ? low[c] : rel >= a.span ? high[c] : table[c][lds_bucket[min(max(rel + a.span, 0), 2 * a.span)]];
+        }
+        s = (word >> r) & 1u ? s : -__builtin_inff();
+        x[c][r] = s;
+        top = fmaxf(top, s);
+      }
+      if (__any(top > most[c])) {
+        asm volatile("");
+        const float now = fmaxf(most[c], top), factor = most[c] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((most[c] - now) * kLog2e);
+        most[c] = now;
+        sum[c] *= factor;
+#pragma unroll
+        for (int s = 0; s < kValueSteps; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[c][s][e] *= factor;
+      }
+      const float base = most[c] == -__builtin_inff() ? 0.f : most[c];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[c][r] = __builtin_amdgcn_exp2f((x[c][r] - base) * kLog2e);
+        sum[c] += x[c][r];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int s = 0; s < kValueSteps; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < kGroups; ++c) acc[c][s][e] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[r][s][e], x[c][r], acc[c][s][e], 0, 0, 0);
+    if (t + kAttnWaves < end) load_values(t + kAttnWaves);
+  }
+
+  // the sets' parts, in LDS: [16][ROWS][D] sums (rows 4 elements apart from a multiple of the banks), [16][ROWS][2] statistics
+  constexpr int kPitch = kValueSteps * 64 + 4;
+  __syncthreads();
+  float* lds_acc = reinterpret_cast<float*>(lds_raw);
+  float* lds_stat = lds_acc + kSets * ROWS * kPitch;
+  const int set = wave * 4 + g;
+#pragma unroll
+  for (int c = 0; c < kGroups; ++c) {
+#pragma unroll
+    for (int s = 0; s < kValueSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 v = {acc[c][s][0][j], acc[c][s][1][j], acc[c][s][2][j], acc[c][s][3][j]};
+        *reinterpret_cast<f32x4*>(lds_acc + (set * ROWS + 4 * c + i) * kPitch + 64 * s + 16 * u + 4 * j) = v;
+      }
+    if (u == 0) {
+      lds_stat[(set * ROWS + 4 * c + i) * 2] = most[c];
+      lds_stat[(set * ROWS + 4 * c + i) * 2 + 1] = sum[c];
+    }
+  }
+  __syncthreads();
+  token_finish<T, ROWS, kSets, kPitch>(a, at, lds_acc, lds_stat, 0.f, tid);
+}
+
+// Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s.  A wave per row: 16 lanes with four neighbouring elements each
+// for every fourth part, then the four sums.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (flat >= rows) return;
-  const int lane = threadIdx.x & 15;
-  float most = -__builtin_inff(), nan = 0.f;
-  for (int s = lane; s < a.splits; s += 16) {
-    const float l = a.part_lse[s * rows + flat];
-    nan += l != l ? 1.f : 0.f;
-    most = fmaxf(most, l);
-  }
+  const int lane = threadIdx.x & 63, quarter = lane >> 4;
+  // up to 64 parts, one to a lane
+  const float mine = lane < a.splits ? a.part_lse[lane * rows + flat] : -__builtin_inff();
+  float most = mine;
 #pragma unroll
-  for (int i = 1; i < 16; i <<= 1) {
-    most = fmaxf(most, __shfl_xor(most, i));
-    nan += __shfl_xor(nan, i);
-  }
-  float total = 0.f;
-  for (int s = lane; s < a.splits && most != -__builtin_inff(); s += 16) total += __builtin_amdgcn_exp2f((a.part_lse[s * rows + flat] - most) * kLog2e);
+  for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+  const float share = mine == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((mine - most) * kLog2e);
+  float total = share;
 #pragma unroll
-  for (int i = 1; i < 16; i <<= 1) total += __shfl_xor(total, i);
-  const float lse = nan > 0.f ? __builtin_nanf("") : most == -__builtin_inff() ? most : most + __builtin_amdgcn_logf(total) * kLn2;
+  for (int i = 32; i; i >>= 1) total += __shfl_xor(total, i);
+  const float lse = total == 0.f ? -__builtin_inff() : most + __builtin_amdgcn_logf(total) * kLn2;     // (a part of NaN makes NaN of the total)
+  const float weight = total == 0.f ? 0.f : share / total;
   const int i = (int)(flat % a.m);
   const int64_t bh = flat / a.m;
   const int h = (int)(bh % a.heads);
   T* O = static_cast<T*>(a.O) + bh / a.heads * a.o.batch + h * a.o.head + (int64_t)i * a.o.row;
-  for (int c = lane * 4; c < a.d; c += 64) {
+  for (int c0 = 0; c0 < a.d; c0 += 64) {                  // every lane stays: the others read its weight
+    const int c = c0 + lane % 16 * 4;
     f32x4 value = {};
 #pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-      const float l = a.part_lse[s * rows + flat];
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+      const int s = min(s0 + quarter, a.splits - 1);
+      const float there = __shfl(weight, s), w = s0 + quarter < a.splits ? there : 0.f;
       const f32x4 v = attn_load_piece<float>(a.part + (s * rows + flat) * a.d, c, a.d);
-      const float f = __builtin_amdgcn_exp2f((l - lse) * kLog2e);
-      if (l != -__builtin_inff()) value += f * v;
+      if (w != 0.f) value += w * v;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < a.d) O[c + e] = (T)value[e];
+    for (int e = 0; e < 4; ++e) {
+      value[e] += __shfl_xor(value[e], 16);
+      value[e] += __shfl_xor(value[e], 32);
+      if (quarter == 0 && c + e < a.d) O[c + e] = (T)value[e];
+    }
   }
   if (lane == 0 && a.lse) a.lse[flat] = lse;
 }
@@ -456,16 +624,22 @@ __global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands
     float most = 0.f;
     if (o.most) {
       most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
-    } else {                                              // few numbers: every wave looks at all of them
+    } else {                                              // few numbers: every workgroup looks at all of them
       const int pieces = (o.d + 3) / 4;
 #pragma unroll 4
-      for (int64_t at = lane; at < rows * pieces; at += 64) {
+      for (int64_t at = threadIdx.x; at < rows * pieces; at += 256) {
         const int64_t row = at / pieces;
         most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, row), (int)(at - row * pieces) * 4, o.d));
       }
     }
 #pragma unroll
     for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+    if (!o.most) {
+      __shared__ float waves[4];
+      if (lane == 0) waves[threadIdx.x >> 6] = most;
+      __syncthreads();
+      most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    }
     const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
     const float factor = ldexpf(1.f, e);
     if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + which] = ldexpf(1.f, -e);
