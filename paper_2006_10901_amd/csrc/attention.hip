@@ -63,7 +63,7 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   const bool f32 = elem_bytes == 4;
   const int least_forward = f32 ? 1 : 4, least_backward = f32 ? 1 : 2;
   if (x.token) {
-    x.token_rows = !f32 ? 32 : group * p.m <= 4 ? 4 : group * p.m <= 8 ? 8 : 16;
+    x.token_rows = group * p.m <= 4 ? 4 : !f32 ? 32 : group * p.m <= 8 ? 8 : 16;
     x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, x.token_rows);
     x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 2, f32 ? 4 : 8);
   } else {
@@ -216,14 +216,18 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
     const int64_t blocks = x.forward_blocks * a.splits;
     if constexpr (sizeof(T) == 2) {
       // K and V of four waves, later their parts
-      const int lds = std::max(kAttnWaves * 2 * 32 * AttnTile<D, 1>::kPitch + bias, kAttnWaves * 32 * (D + 1 + 2) * 4);
-      return launch(attention_token_kernel<D, BIAS>, blocks, lds, a, stream);
-    } else {
-      const int lds = std::max(bias, 4 * kAttnWaves * x.token_rows * ((D + 63) / 64 * 64 + 4 + 2) * 4);
-      return x.token_rows == 4   ? launch(attention_token_f32_kernel<D, 4, BIAS>, blocks, lds, a, stream)
-             : x.token_rows == 8 ? launch(attention_token_f32_kernel<D, 8, BIAS>, blocks, lds, a, stream)
-                                 : launch(attention_token_f32_kernel<D, 16, BIAS>, blocks, lds, a, stream);
+      if (x.token_rows == 32) {
+        const int lds = std::max(kAttnWaves * 2 * 32 * AttnTile<D, 1>::kPitch + bias, kAttnWaves * 32 * (D + 1 + 2) * 4);
+        return launch(attention_tokens_kernel<D, BIAS>, blocks, lds, a, stream);
+      }
     }
+    constexpr int kColumns = 256 / sizeof(T);
+    const int lds = std::max(bias, kAttnWaves * x.token_rows * ((D + kColumns - 1) / kColumns * kColumns + 4 + 2) * 4);
+    if constexpr (sizeof(T) == 4) {
+      if (x.token_rows == 8) return launch(attention_token_kernel<T, D, 8, BIAS>, blocks, lds, a, stream);
+      if (x.token_rows == 16) return launch(attention_token_kernel<T, D, 16, BIAS>, blocks, lds, a, stream);
+    }
+    return launch(attention_token_kernel<T, D, 4, BIAS>, blocks, lds, a, stream);
   }
   if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
   using Tile = AttnTile<D, attn_terms<T>()>;

@@ -136,13 +136,20 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
       }
     }
   }
-  // the same for any d
-  __device__ __forceinline__ void load_any(const T* base, int64_t stride, int rows, int d, int tid) {
-    if (d % kElements == 0) return load(base, stride, rows, d, tid);
+  // the same for any d (one branch around all loads: with one around each, each would be waited for)
+  __device__ __forceinline__ void load_block(const T* base, int64_t stride, int rows, int d, int tid) {
+    if (d % kElements == 0) {
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) {
-      const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
-      v[i] = attn_load_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d);
+      for (int i = 0; i < kCount; ++i) {
+        const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces * kElements;
+        v[i] = attn_load_whole_piece<T>(base + min(row, rows - 1) * stride, c, d);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) {
+        const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces * kElements;
+        v[i] = attn_load_piece<T>(base + min(row, rows - 1) * stride, c, d);
+      }
     }
   }
   __device__ __forceinline__ void store(char* lds, int tid) const {
@@ -372,9 +379,9 @@ struct AttnPanelOf {
   }
 };
 __device__ __forceinline__ void attn_tiles_of_split(const AttnArgs& a, int split, int seen, int& begin, int& end) {
-  const int all = (a.k + kAttnTile - 1) / kAttnTile;
+  const int all = (seen + kAttnTile - 1) / kAttnTile;
   begin = (int)((int64_t)all * split / a.splits);
-  end = min((int)((int64_t)all * (split + 1) / a.splits), (seen + kAttnTile - 1) / kAttnTile);
+  end = (int)((int64_t)all * (split + 1) / a.splits);
 }
 
 // The tiles in which a panel of 128 rows (two sets of 64) sees anything.

@@ -121,13 +121,11 @@ template <int ROWS> struct TokenPanel {
   __device__ __forceinline__ TokenPanel(const AttnArgs& a) {
     rows = a.group * a.m;
     const int panels = (rows + ROWS - 1) / ROWS;
-    int work = blockIdx.x;
-    split = work % a.splits;
-    work /= a.splits;
-    panel = work % panels;
-    work /= panels;
-    kv_head = work % a.kv_heads;
-    batch = work / a.kv_heads;
+    const AttnPlace at(a, panels * a.splits);
+    split = at.piece % a.splits;
+    panel = at.piece / a.splits;
+    kv_head = at.kv_head;
+    batch = at.batch;
   }
 };
 
@@ -172,11 +170,10 @@ template <int N> __device__ __forceinline__ float token_rotate(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
 }
 
-// A few queries: the rows of a head of K and V are those of all query heads that share it, m of each, 32 to a workgroup.  K and V are
-// read once per 32 rows.  The four waves take blocks of 32 keys in turn, each with its own statistics, and no wave waits for another
+// More than 4 rows of a head of K and V, in half precision: 32 to a workgroup.  K and V are read once per 32 rows.  The four waves take blocks of 32 keys in turn, each with its own statistics, and no wave waits for another
 // before the end.
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attention_tokens_kernel(const AttnArgs a) {
   using T = _Float16;
   using Tile = AttnTile<D, 1>;
   constexpr int kBlock = 32 * Tile::kPitch;              // 32 keys or values of a wave
@@ -192,9 +189,8 @@ __global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs 
   const int rows = at.rows, split = at.split, panel = at.panel, batch = at.batch, kv_head = at.kv_head;
 
   const int seen = a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k;
-  const int blocks_all = (a.k + 31) / 32;
-  const int begin = (int)((int64_t)blocks_all * split / a.splits);
-  const int end = min((int)((int64_t)blocks_all * (split + 1) / a.splits), (seen + 31) / 32);
+  const int blocks_all = (seen + 31) / 32;
+  const int begin = (int)((int64_t)blocks_all * split / a.splits), end = (int)((int64_t)blocks_all * (split + 1) / a.splits);
   const int packed = panel * 32 + (lane & 31);
   const bool valid = packed < rows;
   const int of_group = valid ? packed / a.m : 0, row = valid ? packed - of_group * a.m : 0;
@@ -209,8 +205,8 @@ __global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs 
   AttnStage<T, 32, Tile::kBytes, Tile::kPitch, 64> stage_k, stage_v;
   int t = begin + wave;
   if (t < end) {
-    stage_k.load_any(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
-    stage_v.load_any(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
+    stage_k.load_block(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
+    stage_v.load_block(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
   }
   AttnOwn<D, 1> q;
 #pragma unroll
@@ -246,8 +242,8 @@ __global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs 
     const int key0 = t * 32;
     t += kAttnWaves;
     if (t < end) {
-      stage_k.load_any(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
-      stage_v.load_any(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
+      stage_k.load_block(K + (int64_t)t * 32 * a.kk.row, a.kk.row, seen - t * 32, a.d, lane);
+      stage_v.load_block(V + (int64_t)t * 32 * a.v.row, a.v.row, seen - t * 32, a.d, lane);
     }
     unsigned word = ~0u;
     if (a.mask) word = valid ? (unsigned)(a.mask[lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 + row] >> (key0 & 32)) : 0u;
@@ -287,66 +283,120 @@ __global__ __launch_bounds__(256, 2) void attention_token_kernel(const AttnArgs 
   token_finish<T, 32, kAttnWaves, D + 1>(a, at, lds_acc, lds_stat, kOffset, tid);
 }
 
-// The same in single precision, whose products are made as they are, by instructions that multiply 4 x 1 by 1 x 4 numbers in each
-// of sixteen blocks (fp32 instructions of 32 x 32 would do eight times the work for up to four rows, and took 54 us where this takes MEASURED).
+// x += 16 keys by 4 rows, 16 bytes of columns for each lane
+__device__ __forceinline__ void token_scores(f32x4& x, const f32x4& k, const f32x4& q) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_4x4x1f32(k[e], q[e], x, 0, 0, 0);
+}
+__device__ __forceinline__ void token_scores(f32x4& x, const f16x8& k, const f16x8& q) {
+  x = __builtin_amdgcn_mfma_f32_4x4x4f16(__builtin_shufflevector(k, k, 0, 1, 2, 3), __builtin_shufflevector(q, q, 0, 1, 2, 3), x, 0, 0, 0);
+  x = __builtin_amdgcn_mfma_f32_4x4x4f16(__builtin_shufflevector(k, k, 4, 5, 6, 7), __builtin_shufflevector(q, q, 4, 5, 6, 7), x, 0, 0, 0);
+}
+// acc += columns by 4 rows, over the 16 keys
+template <int GROUPS, int STEPS>
+__device__ __forceinline__ void token_values(f32x4 (&acc)[GROUPS][STEPS][4], const f32x4 (&v)[4][STEPS], const f32x4 (&x)[GROUPS]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < GROUPS; ++c) acc[c][s][e] = __builtin_amdgcn_mfma_f32_4x4x1f32(v[r][s][e], x[c][r], acc[c][s][e], 0, 0, 0);
+}
+template <int GROUPS, int STEPS>
+__device__ __forceinline__ void token_values(f32x4 (&acc)[GROUPS][STEPS][8], const f16x8 (&v)[4][STEPS], const f32x4 (&x)[GROUPS]) {
+  f16x4 p[GROUPS];
+#pragma unroll
+  for (int c = 0; c < GROUPS; ++c) p[c] = f16x4{(_Float16)x[c][0], (_Float16)x[c][1], (_Float16)x[c][2], (_Float16)x[c][3]};
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const f16x4 left = {v[0][s][e], v[1][s][e], v[2][s][e], v[3][s][e]};
+#pragma unroll
+      for (int c = 0; c < GROUPS; ++c) acc[c][s][e] = __builtin_amdgcn_mfma_f32_4x4x4f16(left, p[c], acc[c][s][e], 0, 0, 0);
+    }
+}
+// The four sets of 16 lanes together, in all of them.
+template <typename F> __device__ __forceinline__ float token_sets(float v, F both) {
+  unsigned x = __builtin_bit_cast(unsigned, v);
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = __builtin_bit_cast(unsigned, both(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])));
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return both(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
+// Up to 4 rows of a head of K and V, and any number in single precision, on instructions that multiply 4 rows by 4 columns in each of
+// sixteen blocks (4 x 1 by 1 x 4 fp32 numbers, or 4 x 4 by 4 x 4 fp16 ones): those of 32 x 32 do eight times the work for up to four rows.
 //
 // Lane l is row i = l % 4 of block l / 4 of the left operand and column i of that block of the right one.  Blocks split 16 keys into
-// four sets g = l / 16 of four, and columns into quarters u = l / 4 % 4:
-//   scores: lane l has 16 bytes of key 4 g + i, columns 16 t + 4 u .. + 3, and of row i of Q the same columns.  Register r of the result,
+// four sets g = l / 16 of four, and columns into quarters u = l / 4 % 4; E numbers are 16 bytes:
+//   scores: lane l has 16 bytes of key 4 g + i, columns 4 E s + E u .., and of row i of Q the same columns.  Register r of the result,
 //     added up over the quarters (lanes l, l + 4, l + 8, l + 12), is the score of key 4 g + r and row i;
-//   values: that register, as a weight, is the right operand for key 4 g + r; the left one is element e of lane l's 16 bytes of V, columns
-//     64 t + 16 u + 4 i + e.  Register j of the result is column 64 t + 16 u + 4 j + e and row i, of set g.
-// No number of K or V passes through LDS, all loads are of 64 bytes and more at a time, and each set has statistics of its own.
-// ROWS: rows of the workgroup, four to each group of registers.
-template <int D, int ROWS, bool BIAS>
-__global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_token_f32_kernel(const AttnArgs a) {
-  using T = float;
-  constexpr int kGroups = ROWS / 4, kScoreSteps = D / 16, kValueSteps = (D + 63) / 64, kSets = kAttnWaves * 4;
+//   values: those registers, as weights, are the right operand for keys 4 g + r; the left one are elements e of lane l's 16 bytes of V of
+//     these keys, columns 16 E s + 4 E u + E i + e.  Register j of the result is column 16 E s + 4 E u + E j + e and row i, of set g.
+// No number of K or V passes through LDS, and all loads are of 64 bytes and more at a time: bound by reading K and V (32 sequences of 3000
+// states, 8 heads of 128 in fp32, 786 MB: 134 us, 5.9 TB/s; through LDS and instructions of 32 x 32 200 us).  Each set has statistics
+// of its own.  ROWS: rows of the workgroup, four to each group of registers.
+template <typename T, int D, int ROWS, bool BIAS>
+__global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_token_kernel(const AttnArgs a) {
+  using Piece = typename AttnPiece<T>::Type;
+  constexpr int E = 16 / sizeof(T), kBlocks = sizeof(T) == 2 ? 2 : 1, kGroups = ROWS / 4, kScoreSteps = D / (4 * E), kValueSteps = (D + 16 * E - 1) / (16 * E);
+  constexpr float kWeight = sizeof(T) == 2 ? kOffset : 0.f;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i = lane & 3, g = lane >> 4, u = lane >> 2 & 3;
   const TokenPanel<ROWS> at(a);
   const int batch = at.batch, kv_head = at.kv_head;
   const int seen = attn_seen(a, batch);
-  const int all = (a.k + 15) / 16, begin = (int)((int64_t)all * at.split / a.splits),
-            end = min((int)((int64_t)all * (at.split + 1) / a.splits), (seen + 15) / 16);
+  // in units of 16 keys, kBlocks of which a wave takes at a time
+  const int all = (seen + 16 * kBlocks - 1) / (16 * kBlocks), begin = (int)((int64_t)all * at.split / a.splits) * kBlocks,
+            end = min((int)((int64_t)all * (at.split + 1) / a.splits) * kBlocks, (seen + 15) / 16);
   const T* K = static_cast<const T*>(a.K) + batch * a.kk.batch + kv_head * a.kk.head;
   const T* V = static_cast<const T*>(a.V) + batch * a.v.batch + kv_head * a.v.head;
-  const bool whole = a.d % 4 == 0;
+  const bool whole = a.d % E == 0;
 
-  f32x4 kf[kScoreSteps], vf[4][kValueSteps];
+  Piece kf[kBlocks][kScoreSteps], vf[kBlocks][4][kValueSteps];
   // (rows behind the sequence's last are the last one again, with weights of 0)
+  auto key_row = [&](int key) { return K + (int64_t)min(key, seen - 1) * a.kk.row; };
+  auto value_row = [&](int key) { return V + (int64_t)min(key, seen - 1) * a.v.row; };
+  // (one branch around all loads: with one around each, each would be waited for)
   auto load_keys = [&](int t) {
-    const T* row = K + (int64_t)min(t * 16 + 4 * g + i, seen - 1) * a.kk.row;
     if (whole) {
 #pragma unroll
-      for (int s = 0; s < kScoreSteps; ++s) kf[s] = attn_load_whole_piece<T>(row, 16 * s + 4 * u, a.d);
+      for (int x = 0; x < kBlocks * kScoreSteps; ++x)
+        kf[x / kScoreSteps][x % kScoreSteps] =
+            attn_load_whole_piece<T>(key_row((t + x / kScoreSteps) * 16 + 4 * g + i), 4 * E * (x % kScoreSteps) + E * u, a.d);
     } else {
 #pragma unroll
-      for (int s = 0; s < kScoreSteps; ++s) kf[s] = attn_load_piece<T>(row, 16 * s + 4 * u, a.d);
+      for (int x = 0; x < kBlocks * kScoreSteps; ++x)
+        kf[x / kScoreSteps][x % kScoreSteps] =
+            attn_load_piece<T>(key_row((t + x / kScoreSteps) * 16 + 4 * g + i), 4 * E * (x % kScoreSteps) + E * u, a.d);
     }
   };
   auto load_values = [&](int t) {
     if (whole) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int x = 0; x < kBlocks * 4; ++x)
 #pragma unroll
         for (int s = 0; s < kValueSteps; ++s)
-          vf[r][s] = attn_load_whole_piece<T>(V + (int64_t)min(t * 16 + 4 * g + r, seen - 1) * a.v.row, 64 * s + 16 * u + 4 * i, a.d);
+          vf[x / 4][x % 4][s] = attn_load_whole_piece<T>(value_row((t + x / 4) * 16 + 4 * g + x % 4), 16 * E * s + 4 * E * u + E * i, a.d);
     } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int x = 0; x < kBlocks * 4; ++x)
 #pragma unroll
         for (int s = 0; s < kValueSteps; ++s)
-          vf[r][s] = attn_load_piece<T>(V + (int64_t)min(t * 16 + 4 * g + r, seen - 1) * a.v.row, 64 * s + 16 * u + 4 * i, a.d);
+          vf[x / 4][x % 4][s] = attn_load_piece<T>(value_row((t + x / 4) * 16 + 4 * g + x % 4), 16 * E * s + 4 * E * u + E * i, a.d);
     }
   };
-  int t = begin + wave;
+  constexpr int kStep = kAttnWaves * kBlocks;
+  int t = begin + wave * kBlocks;
   if (t < end) {
     load_keys(t);
     load_values(t);
   }
 
-  f32x4 q[kGroups][kScoreSteps];
+  Piece q[kGroups][kScoreSteps];
   int row[kGroups];
   const float* table[kGroups];
   float low[kGroups], high[kGroups];
@@ -358,7 +408,7 @@ __global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_t
   if (BIAS) {
     const int heads = min(a.group - head0, ROWS);
     const T* from = static_cast<const T*>(a.table) + (int64_t)(kv_head * a.group + head0) * a.buckets;
-    for (int x = tid; x < heads * a.buckets; x += 256) lds_table[x] = from[x];
+    for (int x = tid; x < heads * a.buckets; x += 256) lds_table[x] = (float)from[x];
     for (int x = tid; x < 2 * a.span + 1; x += 256) lds_bucket[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
     first = attn_position(a, batch);
     __syncthreads();
@@ -371,7 +421,7 @@ __global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_t
     row[c] = valid ? packed - of_group * a.m : 0;
     const T* Q = static_cast<const T*>(a.Q) + batch * a.q.batch + (kv_head * a.group + of_group) * a.q.head + (int64_t)row[c] * a.q.row;
 #pragma unroll
-    for (int s = 0; s < kScoreSteps; ++s) q[c][s] = valid ? attn_load_piece<T>(Q, 16 * s + 4 * u, a.d) : f32x4{};
+    for (int s = 0; s < kScoreSteps; ++s) q[c][s] = valid ? attn_load_piece<T>(Q, 4 * E * s + E * u, a.d) : Piece{};
     if (BIAS) {
       table[c] = lds_table + (of_group - head0) * a.buckets;
       low[c] = table[c][lds_bucket[0]], high[c] = table[c][lds_bucket[2 * a.span]];
@@ -379,40 +429,43 @@ __global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_t
   }
   const MaskLayout lay(a.m, a.k);
 
-  f32x4 acc[kGroups][kValueSteps][4] = {};
+  f32x4 acc[kGroups][kValueSteps][E] = {};
   float most[kGroups], sum[kGroups];
 #pragma unroll
   for (int c = 0; c < kGroups; ++c) most[c] = -__builtin_inff(), sum[c] = 0.f;
-  for (; t < end; t += kAttnWaves) {
-    const int key0 = t * 16;
-    f32x4 x[kGroups] = {};
+  for (; t < end; t += kStep) {
+    f32x4 x[kBlocks][kGroups] = {};
 #pragma unroll
-    for (int s = 0; s < kScoreSteps; ++s)
+    for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int s = 0; s < kScoreSteps; ++s)
 #pragma unroll
-        for (int c = 0; c < kGroups; ++c) x[c] = __builtin_amdgcn_mfma_f32_4x4x1f32(kf[s][e], q[c][s][e], x[c], 0, 0, 0);
-    if (t + kAttnWaves < end) load_keys(t + kAttnWaves);
+        for (int c = 0; c < kGroups; ++c) token_scores(x[n][c], kf[n][s], q[c][s]);
+    if (t + kStep < end) load_keys(t + kStep);
 #pragma unroll
     for (int c = 0; c < kGroups; ++c) {
-      unsigned word = attn_low_bits(seen - key0);
-      if (a.mask) word &= (unsigned)(a.mask[lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 + row[c]] >> (key0 & 63));
-      word >>= 4 * g;
       float top = -__builtin_inff();
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float s = x[c][r];
-        s += token_rotate<4>(s);
-        s += token_rotate<8>(s);
-        s *= scale;
-        if (BIAS) {
-          const int rel = key0 + 4 * g + r - first - row[c];
-          // far from the diagonal, where most keys are, the bias is one of two
-          s += rel <= -a.span ? low[c] : rel >= a.span ? high[c] : table[c][lds_bucket[min(max(rel + a.span, 0), 2 * a.span)]];
+      for (int n = 0; n < kBlocks; ++n) {
+        const int key0 = (t + n) * 16;
+        unsigned word = attn_low_bits(seen - key0);
+        if (a.mask && key0 < a.k) word &= (unsigned)(a.mask[lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 + row[c]] >> (key0 & 63));
+        word >>= 4 * g;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float s = x[n][c][r];
+          s += token_rotate<4>(s);
+          s += token_rotate<8>(s);
+          s *= scale;
+          if (BIAS) {
+            const int rel = key0 + 4 * g + r - first - row[c];
+            // far from the diagonal, where most keys are, the bias is one of two
+            s += rel <= -a.span ? low[c] : rel >= a.span ? high[c] : table[c][lds_bucket[min(max(rel + a.span, 0), 2 * a.span)]];
+          }
+          s = (word >> r) & 1u ? s : -__builtin_inff();
+          x[n][c][r] = s;
+          top = fmaxf(top, s);
         }
-        s = (word >> r) & 1u ? s : -__builtin_inff();
-        x[c][r] = s;
-        top = fmaxf(top, s);
       }
       if (__any(top > most[c])) {
         asm volatile("");
@@ -422,48 +475,63 @@ __global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_t
 #pragma unroll
         for (int s = 0; s < kValueSteps; ++s)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[c][s][e] *= factor;
+          for (int e = 0; e < E; ++e) acc[c][s][e] *= factor;
       }
       const float base = most[c] == -__builtin_inff() ? 0.f : most[c];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[c][r] = __builtin_amdgcn_exp2f((x[c][r] - base) * kLog2e);
-        sum[c] += x[c][r];
-      }
+      for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[n][c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][c][r] - base, kLog2e, kWeight));
+          sum[c] += x[n][c][r];
+        }
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int s = 0; s < kValueSteps; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int c = 0; c < kGroups; ++c) acc[c][s][e] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[r][s][e], x[c][r], acc[c][s][e], 0, 0, 0);
-    if (t + kAttnWaves < end) load_values(t + kAttnWaves);
+    for (int n = 0; n < kBlocks; ++n) token_values<kGroups, kValueSteps>(acc, vf[n], x[n]);
+    if (t + kStep < end) load_values(t + kStep);
   }
 
-  // the sets' parts, in LDS: [16][ROWS][D] sums (rows 4 elements apart from a multiple of the banks), [16][ROWS][2] statistics
-  constexpr int kPitch = kValueSteps * 64 + 4;
+  // the four sets of a wave, scaled to their common maximum; then the waves' parts in LDS: [4][ROWS][D] sums (rows 4 elements
+  // apart from a multiple of the banks), [4][ROWS][2] statistics
+  constexpr int kPitch = kValueSteps * 16 * E + 4;
   __syncthreads();
   float* lds_acc = reinterpret_cast<float*>(lds_raw);
-  float* lds_stat = lds_acc + kSets * ROWS * kPitch;
-  const int set = wave * 4 + g;
+  float* lds_stat = lds_acc + kAttnWaves * ROWS * kPitch;
 #pragma unroll
   for (int c = 0; c < kGroups; ++c) {
+    const float top = token_sets(most[c], [](float x, float y) { return fmaxf(x, y); });
+    const float factor = most[c] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((most[c] - top) * kLog2e);
+    const auto plus = [](float x, float y) { return x + y; };
+    // (a set that has seen only NaN has no maximum, and its sums count)
+    const float total = token_sets(sum[c] == sum[c] ? sum[c] * factor : sum[c], plus);
 #pragma unroll
     for (int s = 0; s < kValueSteps; ++s)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4 v = {acc[c][s][0][j], acc[c][s][1][j], acc[c][s][2][j], acc[c][s][3][j]};
-        *reinterpret_cast<f32x4*>(lds_acc + (set * ROWS + 4 * c + i) * kPitch + 64 * s + 16 * u + 4 * j) = v;
-      }
-    if (u == 0) {
-      lds_stat[(set * ROWS + 4 * c + i) * 2] = most[c];
-      lds_stat[(set * ROWS + 4 * c + i) * 2 + 1] = sum[c];
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v = acc[c][s][e][j];
+          acc[c][s][e][j] = token_sets(v == v ? v * factor : v, plus);
+        }
+    // each set stores a register's part of the row
+#pragma unroll
+    for (int s = 0; s < kValueSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (g == j) {
+#pragma unroll
+          for (int e = 0; e < E; e += 4) {
+            const f32x4 v = {acc[c][s][e][j], acc[c][s][e + 1][j], acc[c][s][e + 2][j], acc[c][s][e + 3][j]};
+            *reinterpret_cast<f32x4*>(lds_acc + (wave * ROWS + 4 * c + i) * kPitch + 16 * E * s + 4 * E * u + E * j + e) = v;
+          }
+        }
+    if (lane < 4) {
+      lds_stat[(wave * ROWS + 4 * c + i) * 2] = top;
+      lds_stat[(wave * ROWS + 4 * c + i) * 2 + 1] = total;
     }
   }
   __syncthreads();
-  token_finish<T, ROWS, kSets, kPitch>(a, at, lds_acc, lds_stat, 0.f, tid);
+  token_finish<T, ROWS, kAttnWaves, kPitch>(a, at, lds_acc, lds_stat, kWeight, tid);
 }
 
 // Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s.  A wave per row: 16 lanes with four neighbouring elements each
