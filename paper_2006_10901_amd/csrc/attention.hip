@@ -28,8 +28,8 @@ struct Plan {
   int most_parts;
   // offsets into the workspace, in bytes; the terms of Q, K, V and dO and their factors come first (single precision)
   int64_t most, factors, q16, k16, v16, g16;
-  int64_t forward_part, part_lse, forward_bytes;
-  int64_t delta, weight, ends, part, row_sums, part_bias, backward_bytes;
+  int64_t forward_part, part_sum, forward_again, forward_bytes;
+  int64_t delta, weight, ends, part, row_sums, part_bias, backward_again, backward_bytes;
 };
 
 inline int kernel_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
@@ -92,8 +92,9 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   end = x.token ? 0 : terms;
   if (x.forward_splits > 1) {
     x.forward_part = take(end, x.forward_splits * x.rows * p.d);
-    x.part_lse = take(end, x.forward_splits * x.rows);
+    x.part_sum = take(end, 2 * x.forward_splits * x.rows);
   }
+  if (!x.token) x.forward_again = take(end, x.forward_blocks * x.forward_splits * kAttnWaves);
   x.forward_bytes = end;
   end = terms;
   if (x.copied) x.g16 = take(end, x.rows * numbers);
@@ -105,6 +106,7 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   if (p.buckets > 0) {
     x.part_bias = take(end, x.parts * p.heads * (2 * (int64_t)p.span + 1));
   }
+  x.backward_again = take(end, std::max(x.dq_blocks * x.dq_splits, x.dkv_blocks * x.dkv_splits) * kAttnWaves);
   x.backward_bytes = end;
   return x;
 }
@@ -232,7 +234,9 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
   using Tile = AttnTile<D, attn_terms<T>()>;
   const int lds = Tile::kSets * kAttnTile * (Tile::kPitch + Tile::kPitchT) + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
-  return launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream);
+  a.again = reinterpret_cast<unsigned*>(w + x.forward_again);
+  if (!launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream)) return false;
+  return !a.mask || launch(attention_forward_again_kernel<T>, x.forward_blocks * a.splits, 0, a, stream);
 }
 
 template <typename T, int D, bool BIAS>
@@ -242,10 +246,12 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
   const int64_t pieces = up(a.d, 4);
   float* part = a.part = reinterpret_cast<float*>(w + x.part);
+  a.again = reinterpret_cast<unsigned*>(w + x.backward_again);
   if ((x.dq_blocks > 0 || x.dkv_blocks > 0) && !prepare_operands<T, D>(x, a, w, true, stream)) return false;
   if (x.dq_blocks > 0) {
     a.splits = x.dq_splits;
     if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, kTiles + bias, a, stream)) return false;
+    if (a.mask && !launch(attention_dq_again_kernel<T>, x.dq_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
       if (attn_row_sums<T, BIAS>()) {
         attention_rows_kernel<T, BIAS><<<dim3((unsigned)up(x.rows, 256)), dim3(256), 0, stream>>>(a);
@@ -264,6 +270,7 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   if (x.dkv_blocks > 0) {
     a.splits = x.dkv_splits;
     if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 5 * kAttnTile * 4 + bias, a, stream)) return false;
+    if (a.mask && !launch(attention_dkv_again_kernel<T>, x.dkv_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
       attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(
           a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, nullptr, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
@@ -308,12 +315,15 @@ int attention(const spdl_attention_problem* p, const void* Q, const void* K, con
   a.splits = x.forward_splits;
   char* w = static_cast<char*>(workspace);
   a.part = reinterpret_cast<float*>(w + x.forward_part);
-  a.part_lse = reinterpret_cast<float*>(w + x.part_lse);
+  a.part_sum = reinterpret_cast<float2*>(w + x.part_sum);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (!(table ? dispatch_forward<T, true>(x, a, w, s) : dispatch_forward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (a.splits > 1) {
-    attention_join_kernel<T><<<dim3((unsigned)up(x.rows, 4)), dim3(256), 0, s>>>(a);
+    if (x.rows >= 4096 && a.splits <= 16)
+      attention_join_kernel<T, 16><<<dim3((unsigned)up(x.rows, 16)), dim3(256), 0, s>>>(a);
+    else
+      attention_join_kernel<T, 64><<<dim3((unsigned)up(x.rows, 4)), dim3(256), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   }
   return SPDL_OK;

@@ -57,8 +57,9 @@ struct AttnArgs {
   float* weight;
   float* ends;
   float* part;           // workspace: what splits leave for the join
-  float* part_lse;
+  float2* part_sum;      // and of each row its maximum and its sum relative to that (not lse: beside a maximum of 1e9 the sum would be lost)
   double* row_sums;      // workspace: of every split and row, the sums over its keys
+  unsigned* again;       // workspace, with a mask: of each wave of a panel kernel, which of its rows are not finite
   float* part_bias;      // workspace: sums of dS by relative position, one set of 2 span + 1 per panel
 };
 
@@ -255,6 +256,8 @@ __device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char
     }
   }
 }
+
+__device__ __forceinline__ bool attn_finite(float v) { return fabsf(v) < __builtin_inff(); }
 
 // Lanes l and l + 32 together, in both.
 __device__ __forceinline__ float attn_max_halves(float v) {
@@ -487,6 +490,135 @@ __device__ __forceinline__ void attn_hide(f32x16& x, unsigned word, int half) {
   const unsigned w = word >> (4 * half);
 #pragma unroll
   for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r], -__builtin_inff());
+}
+
+// With a mask, what comes out as Inf or NaN is formed again from the definition, one position at a time: tiles multiply whole rows of V (K,
+// Q, dO) by the zeros of positions that a row does not see, and Inf and NaN times 0 are NaN.  A wave has a row (or a key), its lanes
+// columns l and l + 64.  The panel kernels leave which of a wave's 32 rows are to be formed again, and a kernel of the same grid looks
+// (formed in the panel kernels themselves they cost those 3 to 11 % in registers, whether there was anything to do or not).
+
+// The lanes l and l + 32 whose accumulators are not all finite, as bits of 32 columns.
+template <int BLOCKS> __device__ __forceinline__ unsigned attn_not_finite(const f32x16 (&acc)[BLOCKS], bool also) {
+  bool bad = also;
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad |= !attn_finite(acc[b][r]);
+  const uint64_t lanes = __ballot(bad);
+  return (unsigned)lanes | (unsigned)(lanes >> 32);
+}
+
+struct AttnLane { float a, b; };                          // columns l and l + 64
+template <typename T> __device__ __forceinline__ AttnLane attn_lane_row(const T* row, int d, int lane) {
+  return {lane < d ? (float)row[lane] : 0.f, lane + 64 < d ? (float)row[lane + 64] : 0.f};
+}
+__device__ __forceinline__ float attn_lane_dot(const AttnLane& x, const AttnLane& y) {
+  float s = __builtin_fmaf(x.a, y.a, x.b * y.b);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  return s;
+}
+// Rows of a tensor of the caller's.
+template <typename T> __device__ __forceinline__ const T* attn_row(const void* base, const AttnStrides& s, int batch, int head, int64_t row) {
+  return static_cast<const T*>(base) + batch * s.batch + head * s.head + row * s.row;
+}
+// One score; `product`: Q_i . K_j
+template <typename T> __device__ __forceinline__ float attn_score(const AttnArgs& a, int batch, int head, int row, int key, float product) {
+  float bias = 0.f;
+  if (a.table) {
+    const int rel = key - row - attn_position(a, batch);
+    const int b = a.bucket_of[min(max(rel, -a.span), a.span) + a.span];
+    bias = (float)static_cast<const T*>(a.table)[(int64_t)head * a.buckets + min(max(b, 0), a.buckets - 1)];
+  }
+  return __builtin_fmaf(product, a.scale, bias);
+}
+// f(key) for every key in [begin, end) that a row sees, or f(row) for every row that sees a key.
+template <typename F> __device__ __forceinline__ void attn_each_seen(const uint64_t* words, int64_t stride, int at, int begin, int end, F f) {
+  for (int tile = begin / 64; tile * 64 < end; ++tile) {
+    uint64_t word = words ? words[(int64_t)tile * stride + at] : ~0ull;
+    for (int x = max(begin, tile * 64); x < min(end, tile * 64 + 64); ++x)
+      if ((word >> (x & 63)) & 1) f(x);
+  }
+}
+
+// O over the keys [begin, end) of one row, into `to`; its maximum and its sum relative to that.
+template <typename T, typename OUT>
+__device__ __forceinline__ float2 attn_exact_forward(const AttnArgs& a, int batch, int head, int row, int begin, int end, OUT* to, int lane) {
+  const MaskLayout lay(a.m, a.k);
+  const int kv_head = head / a.group;
+  const AttnLane q = attn_lane_row(attn_row<T>(a.Q, a.q, batch, head, row), a.d, lane);
+  float most = -__builtin_inff(), sum = 0.f;
+  AttnLane o = {0.f, 0.f};
+  attn_each_seen(a.mask ? a.mask + lay.row_words : nullptr, lay.ti * 64, row, begin, end, [&](int key) {
+    if (sum != sum) return;                               // NaN stays NaN
+    const AttnLane k = attn_lane_row(attn_row<T>(a.K, a.kk, batch, kv_head, key), a.d, lane);
+    const float s = attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k));
+    if (s == -__builtin_inff()) return;
+    const AttnLane v = attn_lane_row(attn_row<T>(a.V, a.v, batch, kv_head, key), a.d, lane);
+    const float now = fmaxf(most, s), factor = most == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((most - now) * kLog2e);
+    const float p = __builtin_amdgcn_exp2f((s - now) * kLog2e);
+    most = now;
+    sum = __builtin_fmaf(sum, factor, p);
+    // (a factor of 0 is for nothing summed, or next to nothing)
+    o.a = __builtin_fmaf(p, v.a, factor == 0.f ? 0.f : o.a * factor);
+    o.b = __builtin_fmaf(p, v.b, factor == 0.f ? 0.f : o.b * factor);
+  });
+  const bool none = sum == 0.f;
+  const float inv = none ? 0.f : 1.f / sum;
+  if (lane < a.d) to[lane] = (OUT)(sum != sum ? sum : o.a * inv);
+  if (lane + 64 < a.d) to[lane + 64] = (OUT)(sum != sum ? sum : o.b * inv);
+  return {most, sum};
+}
+// The logarithm of a row's sum; that of a row that sees nothing: -inf.
+__device__ __forceinline__ float attn_lse(float2 s) { return s.y == 0.f ? -__builtin_inff() : s.x + __builtin_amdgcn_logf(s.y) * kLn2; }
+
+// dQ of one row over the keys [begin, end).  weight: what P is taken times.
+template <typename T, typename OUT>
+__device__ __forceinline__ void attn_exact_dq(const AttnArgs& a, int batch, int head, int row, int begin, int end, float lse, float delta, float weight,
+                                              OUT* to, int lane) {
+  const MaskLayout lay(a.m, a.k);
+  const int kv_head = head / a.group;
+  const AttnLane q = attn_lane_row(attn_row<T>(a.Q, a.q, batch, head, row), a.d, lane);
+  const AttnLane g = attn_lane_row(attn_row<T>(a.dO, a.dout, batch, head, row), a.d, lane);
+  AttnLane out = {0.f, 0.f};
+  attn_each_seen(a.mask ? a.mask + lay.row_words : nullptr, lay.ti * 64, row, begin, end, [&](int key) {
+    const AttnLane k = attn_lane_row(attn_row<T>(a.K, a.kk, batch, kv_head, key), a.d, lane);
+    const float p = weight * __builtin_amdgcn_exp2f((attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse) * kLog2e);
+    const float ds = p * (attn_lane_dot(g, attn_lane_row(attn_row<T>(a.V, a.v, batch, kv_head, key), a.d, lane)) - delta);
+    out.a = __builtin_fmaf(ds, k.a, out.a);
+    out.b = __builtin_fmaf(ds, k.b, out.b);
+  });
+  if (lane < a.d) to[lane] = (OUT)(out.a * a.scale);
+  if (lane + 64 < a.d) to[lane + 64] = (OUT)(out.b * a.scale);
+}
+
+// dK and dV of one key over the tiles [begin, end) of all heads of the group (see attention_dkv_kernel).
+template <typename T, typename OUT>
+__device__ __forceinline__ void attn_exact_dkv(const AttnArgs& a, int batch, int kv_head, int key, int64_t begin, int64_t end, OUT* dk_to, OUT* dv_to, int lane) {
+  const MaskLayout lay(a.m, a.k);
+  const int tiles = (a.m + 63) / 64;
+  const AttnLane k = attn_lane_row(attn_row<T>(a.K, a.kk, batch, kv_head, key), a.d, lane);
+  const AttnLane v = attn_lane_row(attn_row<T>(a.V, a.v, batch, kv_head, key), a.d, lane);
+  AttnLane dk = {0.f, 0.f}, dv = {0.f, 0.f};
+  for (int h = 0; h < a.group; ++h) {
+    const int head = kv_head * a.group + h;
+    const int64_t first = (int64_t)h * tiles, from = begin > first ? begin - first : 0, to = end - first < tiles ? end - first : tiles;
+    if (from >= to) continue;
+    attn_each_seen(a.mask ? a.mask + lay.col_words : nullptr, lay.tj * 64, key, (int)from * 64, min((int)to * 64, a.m), [&](int row) {
+      const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
+      const float lse = a.lse[flat];
+      if (lse == -__builtin_inff()) return;
+      const AttnLane q = attn_lane_row(attn_row<T>(a.Q, a.q, batch, head, row), a.d, lane);
+      const AttnLane g = attn_lane_row(attn_row<T>(a.dO, a.dout, batch, head, row), a.d, lane);
+      float p = __builtin_amdgcn_exp2f((attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse) * kLog2e);
+      if (sizeof(T) == 4) p *= a.weight[flat];
+      const float ds = p * (attn_lane_dot(g, v) - a.delta[flat]);
+      dk.a = __builtin_fmaf(ds, q.a, dk.a), dk.b = __builtin_fmaf(ds, q.b, dk.b);
+      dv.a = __builtin_fmaf(p, g.a, dv.a), dv.b = __builtin_fmaf(p, g.b, dv.b);
+    });
+  }
+  if (lane < a.d) dk_to[lane] = (OUT)(dk.a * a.scale), dv_to[lane] = (OUT)dv.a;
+  if (lane + 64 < a.d) dk_to[lane + 64] = (OUT)(dk.b * a.scale), dv_to[lane + 64] = (OUT)dv.b;
 }
 
 }  // namespace spdl

@@ -20,8 +20,13 @@ struct AttnScale {
     for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[r]));
     if (!__any(most > limit * by)) return false;
     asm volatile("");
+    // (a row of Inf makes no room for itself at the expense of the others)
+    most = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = fmaxf(most, attn_finite(x[r]) ? fabsf(x[r]) : 0.f);
 #pragma unroll
     for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if (!(most > limit * by)) return false;
     // 2^11 for the largest here, room for sixteen times as much; powers within +-100, so that the factors at the end are normal
     // numbers (a quotient that is not belongs to sums of less than 2^-126 of what comes)
     const int e = min(max(11 - ilogbf(fminf(most / by, 1e30f)), -100), 100);
@@ -237,7 +242,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     }
   }
 
-  float factor = a.scale * f.k / ds_scale.factor;
+  float weight = 1.f;                                    // what the row's P is taken times
   const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   if constexpr (kSums) {
     double s[kAttnRowSums] = {sums.ds, sums.p, sums.low, sums.low_p, sums.high, sums.high_p};
@@ -245,7 +250,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     for (int i = 0; i < kAttnRowSums; ++i) s[i] += __shfl_xor(s[i], 32);
     const AttnRowSums all = {s[0], s[1], s[2], s[3], s[4], s[5]};
     if (a.splits == 1) {
-      if (sizeof(T) == 4 && all.p > 0. && all.p < 1e30) factor *= (float)(1. / all.p);
+      if (sizeof(T) == 4 && all.p > 0. && all.p < 1e30) weight = (float)(1. / all.p);
       if (valid && half == 0) attn_finish_row<T, BIAS>(a, own.flat, delta, all);
     } else if (valid && half == 0) {
       if (at.split == 0) a.delta[own.flat] = delta;
@@ -257,11 +262,39 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   } else if (valid && half == 0 && at.split == 0) {
     a.delta[own.flat] = delta;
   }
+  if (a.mask) {
+    // (rows whose own numbers are Inf or NaN are right as they are)
+    const unsigned bad = attn_not_finite(acc, false) & (unsigned)__ballot(valid && attn_finite(own.lse) && attn_finite(delta));
+    if (lane == 0) a.again[blockIdx.x * kAttnWaves + wave] = bad;
+  }
+  const float factor = weight * a.scale * f.k / ds_scale.factor;
   if (a.splits == 1) {
     T* dQ = static_cast<T*>(a.dQ) + batch * a.dq.batch + head * a.dq.head + (int64_t)row * a.dq.row;
     attn_store_rows<T, D>(dQ, valid, acc, factor, a.d, half);
   } else {
     attn_store_rows<float, D>(a.part + (at.split * rows + own.flat) * a.d, valid, acc, factor, a.d, half);
+  }
+}
+// Runs before attention_rows_kernel: parts are sums of P as lse gives it, with D as it is then.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dq_again_kernel(const AttnArgs a) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  unsigned left = uniform(a.again[blockIdx.x * kAttnWaves + wave]);
+  if (!left) return;
+  const AttnPanelOf at(a, a.m);
+  int begin, end;
+  const int seen = attn_seen(a, at.batch);
+  attn_tiles_of_split(a, at.split, seen, begin, end);
+  for (; left; left &= left - 1) {
+    const int row = at.panel * kAttnPanel + wave * 32 + __builtin_ctz(left);
+    const int64_t flat = ((int64_t)at.batch * a.heads + at.head) * a.m + row;
+    const float lse = a.lse[flat], delta = a.delta[flat], weight = a.splits == 1 && sizeof(T) == 4 ? a.weight[flat] : 1.f;
+    if (a.splits == 1)
+      attn_exact_dq<T>(a, at.batch, at.head, row, begin * kAttnTile, min(end * kAttnTile, seen), lse, delta, weight,
+                       static_cast<T*>(a.dQ) + at.batch * a.dq.batch + at.head * a.dq.head + (int64_t)row * a.dq.row, lane);
+    else
+      attn_exact_dq<T>(a, at.batch, at.head, row, begin * kAttnTile, min(end * kAttnTile, seen), lse, delta, weight,
+                       a.part + ((int64_t)at.split * a.batch * a.heads * a.m + flat) * a.d, lane);
   }
 }
 
@@ -543,6 +576,10 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   const float offset = __builtin_amdgcn_exp2f(-kOffset);
   const float to_dk = a.scale * f.q * offset / ds_scale.factor, to_dv = f.g * offset;
   const bool stored = key < a.k;
+  if (a.mask) {
+    const unsigned bad = (attn_not_finite(dk, false) | attn_not_finite(dv, false)) & (unsigned)__ballot(valid);
+    if (lane == 0) a.again[blockIdx.x * kAttnWaves + wave] = bad;
+  }
   if (a.splits == 1) {
     T* dK = static_cast<T*>(a.dK) + batch * a.dk.batch + kv_head * a.dk.head + (int64_t)key * a.dk.row;
     T* dV = static_cast<T*>(a.dV) + batch * a.dv.batch + kv_head * a.dv.head + (int64_t)key * a.dv.row;
@@ -552,6 +589,26 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
     const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k, flat = ((int64_t)batch * a.kv_heads + kv_head) * a.k + key;
     attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, stored, dk, to_dk, a.d, half);
     attn_store_rows<float, D>(a.part + ((a.splits + split) * rows + flat) * a.d, stored, dv, to_dv, a.d, half);
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dkv_again_kernel(const AttnArgs a) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  unsigned left = uniform(a.again[blockIdx.x * kAttnWaves + wave]);
+  if (!left) return;
+  const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
+  const AttnPlace place(a, panels * a.splits);
+  const int split = place.piece % a.splits, panel = place.piece / a.splits;
+  const int64_t all = (int64_t)a.group * ((a.m + kAttnTile - 1) / kAttnTile), begin = all * split / a.splits, end = all * (split + 1) / a.splits;
+  for (; left; left &= left - 1) {
+    const int key = panel * kAttnPanel + wave * 32 + __builtin_ctz(left);
+    if (a.splits == 1) {
+      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, static_cast<T*>(a.dK) + place.batch * a.dk.batch + place.kv_head * a.dk.head + (int64_t)key * a.dk.row,
+                        static_cast<T*>(a.dV) + place.batch * a.dv.batch + place.kv_head * a.dv.head + (int64_t)key * a.dv.row, lane);
+    } else {
+      const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k, flat = ((int64_t)place.batch * a.kv_heads + place.kv_head) * a.k + key;
+      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, a.part + (split * rows + flat) * a.d, a.part + ((a.splits + split) * rows + flat) * a.d, lane);
+    }
   }
 }
 

@@ -100,18 +100,45 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   }
 
   const float total = attn_sum_halves(run.sum);
-  const bool none = run.most == -__builtin_inff() && total == 0.f;
-  const float lse = none ? -__builtin_inff() : run.most + (__builtin_amdgcn_logf(total) - kOffset) * kLn2;
+  const bool none = total == 0.f;                        // (a sum of NaN is none)
+  const float2 sum = {run.most, total * __builtin_amdgcn_exp2f(-kOffset)};
   const float inv = none ? 0.f : f.v / total;
+  if (a.mask) {
+    const unsigned bad = attn_not_finite(acc, !attn_finite(total)) & (unsigned)__ballot(valid);
+    if (lane == 0) a.again[blockIdx.x * kAttnWaves + wave] = bad;
+  }
   const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
   if (a.splits == 1) {
     T* O = static_cast<T*>(a.O) + batch * a.o.batch + head * a.o.head + (int64_t)row * a.o.row;
     attn_store_rows<T, D>(O, valid, acc, inv, a.d, half);
-    if (valid && half == 0 && a.lse) a.lse[flat] = lse;
+    if (valid && half == 0 && a.lse) a.lse[flat] = attn_lse(sum);
   } else {
     const int64_t rows = (int64_t)a.batch * a.heads * a.m;
     attn_store_rows<float, D>(a.part + (at.split * rows + flat) * a.d, valid, acc, inv, a.d, half);
-    if (valid && half == 0) a.part_lse[at.split * rows + flat] = lse;
+    if (valid && half == 0) a.part_sum[at.split * rows + flat] = sum;
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void attention_forward_again_kernel(const AttnArgs a) {
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  unsigned left = uniform(a.again[blockIdx.x * kAttnWaves + wave]);
+  if (!left) return;
+  const AttnPanelOf at(a, a.m);
+  int begin, end;
+  const int seen = attn_seen(a, at.batch);
+  attn_tiles_of_split(a, at.split, seen, begin, end);
+  const int64_t flat0 = ((int64_t)at.batch * a.heads + at.head) * a.m, part0 = (int64_t)at.split * a.batch * a.heads * a.m + flat0;
+  for (; left; left &= left - 1) {
+    const int row = at.panel * kAttnPanel + wave * 32 + __builtin_ctz(left);
+    const int last = min(end * kAttnTile, seen);
+    if (a.splits == 1) {
+      const float2 sum = attn_exact_forward<T>(a, at.batch, at.head, row, begin * kAttnTile, last,
+                                               static_cast<T*>(a.O) + at.batch * a.o.batch + at.head * a.o.head + (int64_t)row * a.o.row, lane);
+      if (lane == 0 && a.lse) a.lse[flat0 + row] = attn_lse(sum);
+    } else {
+      const float2 sum = attn_exact_forward<T>(a, at.batch, at.head, row, begin * kAttnTile, last, a.part + (part0 + row) * a.d, lane);
+      if (lane == 0) a.part_sum[part0 + row] = sum;
+    }
   }
 }
 
@@ -132,7 +159,13 @@ template <int ROWS> struct TokenPanel {
 // Joins PARTS parts of the keys that lie in LDS, each with its own maximum and sum: each is scaled to the common maximum, then they are
 // added up in their order.  offset: the power of two that weights were taken times.
 template <typename T, int ROWS, int PARTS, int PITCH>
-__device__ __forceinline__ void token_finish(const AttnArgs& a, const TokenPanel<ROWS>& at, const float* parts, const float* stats, float offset, int tid) {
+__device__ __forceinline__ void token_finish(const AttnArgs& a, const TokenPanel<ROWS>& at, const float* parts, const float* stats, float offset, int begin,
+                                             int end, int tid) {
+  __shared__ unsigned bad;                               // with a mask: rows with a result that is not finite
+  if (a.mask) {
+    if (tid == 0) bad = 0;
+    __syncthreads();
+  }
   const int64_t all = (int64_t)a.batch * a.heads * a.m;
   for (int x = tid; x < ROWS * a.d; x += 256) {
     const int r = x / a.d, col = x - r * a.d, p = at.panel * ROWS + r;
@@ -151,16 +184,34 @@ __device__ __forceinline__ void token_finish(const AttnArgs& a, const TokenPanel
       total += s == s ? s * f : s;
       value += v == v ? v * f : v;
     }
-    const bool none = most == -__builtin_inff() && total == 0.f;
-    const float lse = none ? -__builtin_inff() : most + (__builtin_amdgcn_logf(total) - offset) * kLn2;
-    const float result = none ? 0.f : value / total;
+    const float result = total == 0.f ? 0.f : value / total;
+    if (a.mask && (!attn_finite(result) || !attn_finite(total))) {
+      atomicOr(&bad, 1u << r);
+      continue;
+    }
+    const float2 sum = {most, total * __builtin_amdgcn_exp2f(-offset)};
     const int64_t flat = ((int64_t)at.batch * a.heads + h) * a.m + i;
     if (a.splits == 1) {
       (static_cast<T*>(a.O) + at.batch * a.o.batch + h * a.o.head + (int64_t)i * a.o.row)[col] = (T)result;
-      if (col == 0 && a.lse) a.lse[flat] = lse;
+      if (col == 0 && a.lse) a.lse[flat] = attn_lse(sum);
     } else {
       a.part[(at.split * all + flat) * a.d + col] = result;
-      if (col == 0) a.part_lse[at.split * all + flat] = lse;
+      if (col == 0) a.part_sum[at.split * all + flat] = sum;
+    }
+  }
+  if (!a.mask) return;
+  __syncthreads();
+  for (unsigned left = uniform(bad); left; left &= left - 1) {
+    const int r = __builtin_ctz(left), p = at.panel * ROWS + r, g = p / a.m, i = p - g * a.m, h = at.kv_head * a.group + g;
+    if (r % kAttnWaves != uniform(tid >> 6)) continue;
+    const int64_t flat = ((int64_t)at.batch * a.heads + h) * a.m + i;
+    if (a.splits == 1) {
+      const float2 sum = attn_exact_forward<T>(a, at.batch, h, i, begin, end,
+                                               static_cast<T*>(a.O) + at.batch * a.o.batch + h * a.o.head + (int64_t)i * a.o.row, tid & 63);
+      if ((tid & 63) == 0 && a.lse) a.lse[flat] = attn_lse(sum);
+    } else {
+      const float2 sum = attn_exact_forward<T>(a, at.batch, h, i, begin, end, a.part + (at.split * all + flat) * a.d, tid & 63);
+      if ((tid & 63) == 0) a.part_sum[at.split * all + flat] = sum;
     }
   }
 }
@@ -280,7 +331,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attention_tokens_kernel(
     lds_stat[(wave * 32 + lane) * 2 + 1] = sum;
   }
   __syncthreads();
-  token_finish<T, 32, kAttnWaves, D + 1>(a, at, lds_acc, lds_stat, kOffset, tid);
+  token_finish<T, 32, kAttnWaves, D + 1>(a, at, lds_acc, lds_stat, kOffset, begin * 32, min(end * 32, seen), tid);
 }
 
 // x += 16 keys by 4 rows, 16 bytes of columns for each lane
@@ -531,26 +582,27 @@ __global__ __launch_bounds__(256, D <= 64 || ROWS <= 8 ? 2 : 1) void attention_t
     }
   }
   __syncthreads();
-  token_finish<T, ROWS, kAttnWaves, kPitch>(a, at, lds_acc, lds_stat, kWeight, tid);
+  token_finish<T, ROWS, kAttnWaves, kPitch>(a, at, lds_acc, lds_stat, kWeight, begin * 16, min(end * 16, seen), tid);
 }
 
-// Joins what the parts of the keys gave: O = sum of exp(lse_s - lse) O_s.  A wave per row: 16 lanes with four neighbouring elements each
-// for every fourth part, then the four sums.
-template <typename T>
+// Joins what the parts of the keys gave, by their sums.  16 lanes have four neighbouring elements each of a row; a row
+// has LANES: where there are few rows, the 64 lanes of a wave, each 16 of which take every fourth part, else 16 (us, 64 and 16 lanes:
+// 32768 rows of 64 columns, two parts 15.7 and 8.7; 8 rows of 128, 31 parts 10 and 13).  At most LANES parts.
+template <typename T, int LANES>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kTurns = LANES / 16;
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (flat >= rows) return;
-  const int lane = threadIdx.x & 63, quarter = lane >> 4;
-  // up to 64 parts, one to a lane
-  const float mine = lane < a.splits ? a.part_lse[lane * rows + flat] : -__builtin_inff();
-  float most = mine;
+  const int lane = threadIdx.x % LANES, turn = lane >> 4;
+  const float2 mine = lane < a.splits ? a.part_sum[lane * rows + flat] : float2{-__builtin_inff(), 0.f};
+  float most = mine.x;
 #pragma unroll
-  for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
-  const float share = mine == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((mine - most) * kLog2e);
+  for (int i = LANES / 2; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+  // (a part that has seen only NaN has no maximum, and its sum counts)
+  const float share = mine.x == -__builtin_inff() ? mine.y : mine.y * __builtin_amdgcn_exp2f((mine.x - most) * kLog2e);
   float total = share;
 #pragma unroll
-  for (int i = 32; i; i >>= 1) total += __shfl_xor(total, i);
-  const float lse = total == 0.f ? -__builtin_inff() : most + __builtin_amdgcn_logf(total) * kLn2;     // (a part of NaN makes NaN of the total)
+  for (int i = LANES / 2; i; i >>= 1) total += __shfl_xor(total, i);
   const float weight = total == 0.f ? 0.f : share / total;
   const int i = (int)(flat % a.m);
   const int64_t bh = flat / a.m;
@@ -559,21 +611,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
   for (int c0 = 0; c0 < a.d; c0 += 64) {                  // every lane stays: the others read its weight
     const int c = c0 + lane % 16 * 4;
     f32x4 value = {};
-#pragma unroll 4
-    for (int s0 = 0; s0 < a.splits; s0 += 4) {
-      const int s = min(s0 + quarter, a.splits - 1);
-      const float there = __shfl(weight, s), w = s0 + quarter < a.splits ? there : 0.f;
+    for (int s0 = 0; s0 < a.splits; s0 += kTurns) {
+      const int s = min(s0 + turn, a.splits - 1);
+      const float there = __shfl(weight, s, LANES), w = s0 + turn < a.splits ? there : 0.f;
       const f32x4 v = attn_load_piece<float>(a.part + (s * rows + flat) * a.d, c, a.d);
       if (w != 0.f) value += w * v;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      value[e] += __shfl_xor(value[e], 16);
-      value[e] += __shfl_xor(value[e], 32);
-      if (quarter == 0 && c + e < a.d) O[c + e] = (T)value[e];
+      if constexpr (LANES == 64) {
+        value[e] += __shfl_xor(value[e], 16);
+        value[e] += __shfl_xor(value[e], 32);
+      }
+      if (turn == 0 && c + e < a.d) O[c + e] = (T)value[e];
     }
   }
-  if (lane == 0 && a.lse) a.lse[flat] = lse;
+  if (lane == 0 && a.lse) a.lse[flat] = attn_lse({most, total});
 }
 
 // Bits of the sparse matrix, from its CSR topology: cleared, the words by rows set by one wave per row (which thread sets a bit first changes
