@@ -9,6 +9,7 @@
 #include "attention_backward.hpp"
 #include "attention_forward.hpp"
 
+
 namespace {
 
 using namespace spdl;
@@ -24,7 +25,7 @@ struct Plan {
   int64_t rows, kv_rows, parts;        // parts: workgroups that leave sums of dS per head
   int width;                           // d rounded up to the width of a kernel
   bool copied;                         // whether the panel kernels take copies of Q, K, V and dO: fp16 terms of fp32 numbers, or rows
-                                       // of whole 16-byte pieces where the caller's are not
+                                       // of whole 16-byte pieces where the caller's are not, or lie 2^24 elements apart
   int most_parts;
   // offsets into the workspace, in bytes; the terms of Q, K, V and dO and their factors come first (single precision)
   int64_t most, factors, q16, k16, v16, g16;
@@ -43,9 +44,10 @@ inline int64_t take(int64_t& end, int64_t floats) {
   return at;
 }
 
-// How many workgroups a panel's work is split over: enough to give every compute unit `want` of them, of at least `least` steps each.
-inline int split_count(int64_t blocks, int64_t steps, int want, int least) {
-  if (blocks <= 0 || steps <= 2 * least) return 1;
+// How many workgroups a panel's work is split over: enough to give every compute unit `want` of them, of at least `least` steps each, if
+// there are `from` steps, so that what is saved pays for the kernel that joins the parts.
+inline int split_count(int64_t blocks, int64_t steps, int want, int least, int from) {
+  if (blocks <= 0 || steps < from) return 1;
   const int64_t s = std::min<int64_t>(want * 256 / blocks, steps / least);
   return (int)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
@@ -57,30 +59,31 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   x.kv_rows = (int64_t)p.batch * p.kv_heads * p.k;
   x.width = kernel_width(p.d);
   x.token = p.m <= 16;
-  // Least steps per part: what a part saves has to pay for the kernel that joins (us, 1 / 2 / 4 steps: fp32 training step of 3 x 6 heads of 77 x 203 85 / 95 / 117,
-  // fp16 training step of 8 x 8 heads of 289 x 209 57 / 45 / 45, fp16 forward of 5 x 2 heads of 162 x 1242 16.0 / 14.6 / 14.2; single tokens, 4 / 8
-  // blocks of 32 keys: fp32 2 x 4 heads on 361 keys 18 / 26, fp16 7 x 14 rows on 3547 keys 23 / 19).
+  // Tiles of 64 keys (or queries) per part at least, and from how many on a panel is split: a tile takes 2 to 4 us where a compute unit has one
+  // workgroup, the kernel that joins the parts 4 (us, 1 / 2 / 4 tiles per part: fp32 training step of 3 x 6 heads of 77 x 203 85 / 95 / 117, fp16 one of
+  // 2 heads of 22 x 1505 65 / 62 / 67; single tokens, 4 / 8 blocks of 32 keys: fp32 2 x 4 heads on 361 keys 18 / 26, fp16 7 x 14 rows on 3547 23 / 19).
   const bool f32 = elem_bytes == 4;
-  const int least_forward = f32 ? 1 : 4, least_backward = f32 ? 1 : 2;
+  const int least = f32 ? 1 : 2, from = f32 ? 3 : 6;
   if (x.token) {
     x.token_rows = group * p.m <= 4 ? 4 : !f32 ? 32 : group * p.m <= 8 ? 8 : 16;
     x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, x.token_rows);
-    x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 2, f32 ? 4 : 8);
+    x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 2, f32 ? 4 : 8, f32 ? 9 : 17);
   } else {
     x.forward_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), 2, least_forward);
+    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), 2, least, from);
   }
   x.dq_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, least_backward);
+  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, least, from);
   x.dkv_blocks = (int64_t)p.batch * p.kv_heads * up(p.k, kAttnPanel);
-  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, least_backward);
+  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, least, from);
   // tiles near the diagonal that a panel meets
-  x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 1);
+  x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 1, 3);
   x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dbias_splits;
   x.most_parts = (int)std::min<int64_t>(64, std::max<int64_t>(1, up(std::max<int64_t>(group * p.m, p.k), 64)));
 
   int64_t terms = 0, end = 0;
-  x.copied = elem_bytes == 4 || p.d % 8 != 0;
+  const int64_t longest = std::max(std::max(p.Q.row, p.K.row), std::max(p.V.row, p.dO.row));
+  x.copied = elem_bytes == 4 || p.d % 8 != 0 || longest >= 1 << 24;
   const int numbers = elem_bytes == 4 ? x.width : x.width / 2;    // floats' room that a row of terms takes
   if (x.copied) {
     x.most = take(terms, (int64_t)p.batch * p.kv_heads * 4 * x.most_parts);
@@ -253,17 +256,12 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
     if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, kTiles + bias, a, stream)) return false;
     if (a.mask && !launch(attention_dq_again_kernel<T>, x.dq_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
-      if (attn_row_sums<T, BIAS>()) {
-        attention_rows_kernel<T, BIAS><<<dim3((unsigned)up(x.rows, 256)), dim3(256), 0, stream>>>(a);
-        if (hipGetLastError() != hipSuccess) return false;
-      }
-      attention_sum_kernel<T><<<dim3((unsigned)up(x.rows * pieces, 256)), dim3(256), 0, stream>>>(
-          a.splits, x.rows, a.heads, a.m, a.d, part, sizeof(T) == 4 ? a.weight : nullptr, AttnSum{a.dq, a.dQ}, AttnSum{});
+      attention_sum_dq_kernel<T, BIAS, attn_row_sums<T, BIAS>()><<<dim3((unsigned)up(x.rows * pieces, 256)), dim3(256), 0, stream>>>(a);
       if (hipGetLastError() != hipSuccess) return false;
     }
     if (BIAS && a.part_bias) {
       a.splits = x.dbias_splits;
-      const int lds = kTiles + bias + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
+      const int lds = kTiles + bias + 16 + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
       if (!launch(attention_dbias_kernel<T, D>, x.dq_blocks * a.splits, lds, a, stream)) return false;
     }
   }
@@ -273,7 +271,7 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
     if (a.mask && !launch(attention_dkv_again_kernel<T>, x.dkv_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
       attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(
-          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, nullptr, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
+          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
       if (hipGetLastError() != hipSuccess) return false;
     }
   }
@@ -358,7 +356,8 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   (void)hipGetLastError();
   if (!(table ? dispatch_backward<T, true>(x, a, w, s) : dispatch_backward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
   if (dtable) {
-    attention_dtable_kernel<T><<<dim3((unsigned)p->heads), dim3(1024), (2 * p->span + 1) * 12, s>>>(a, (int)x.parts, static_cast<T*>(dtable));
+    const int n = 2 * p->span + 1;
+    attention_dtable_kernel<T><<<dim3((unsigned)p->heads), dim3(1024), (n < 1024 ? 1024 / n : 1) * n * 8 + n * 4, s>>>(a, (int)x.parts, static_cast<T*>(dtable));
     if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   }
   return SPDL_OK;

@@ -121,19 +121,31 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
   static_assert(ROWS * kPieces % THREADS == 0, "whole pieces per thread");
   Piece v[kCount];
   // rows [0, rows) of `base`, `stride` elements apart, of d elements, a multiple of a piece's (rows >= 1); behind them the last one again,
-  // whose weights are 0 there
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d, int tid) {
+  // whose weights are 0 there.  ROWS rows span less than 2^31 bytes: a whole tile takes one offset per thread and bases that are the
+  // workgroup's, no arithmetic of the lanes (with 64-bit products per piece it took a third of their instructions).
+  // (Rows of 12 and 24 pieces, which do not divide the threads: an offset per piece.)
+  static constexpr bool kEven = THREADS % kPieces == 0;
+  struct Offsets { unsigned v[kEven ? 1 : kCount]; };
+  static __device__ __forceinline__ Offsets whole_offsets(int64_t stride, int tid) {
+    Offsets o;
+#pragma unroll
+    for (int i = 0; i < (kEven ? 1 : kCount); ++i)
+      o.v[i] = (unsigned)((i * THREADS + tid) / kPieces) * (unsigned)(stride * (int)sizeof(T)) + (i * THREADS + tid) % kPieces * 16;
+    return o;
+  }
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d, const Offsets& whole, int tid) {
+    const char* from = reinterpret_cast<const char*>(base);
     if (rows >= ROWS && d * (int)sizeof(T) == BYTES) {
 #pragma unroll
-      for (int i = 0; i < kCount; ++i) {
-        const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
-        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(base + row * stride + c * kElements);
-      }
+      for (int i = 0; i < kCount; ++i)
+        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(from + (kEven ? i * (THREADS / kPieces) * stride * (int)sizeof(T) : 0) + whole.v[kEven ? 0 : i]);
     } else {
+      asm volatile("");
 #pragma unroll
       for (int i = 0; i < kCount; ++i) {
         const int at = i * THREADS + tid, row = at / kPieces, c = at % kPieces;
-        v[i] = attn_load_whole_piece<T>(base + min(row, rows - 1) * stride, c * kElements, d);
+        const unsigned offset = (unsigned)min(row, rows - 1) * (unsigned)(stride * (int)sizeof(T)) + min(c * kElements, d - kElements) * (int)sizeof(T);
+        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(from + offset);
       }
     }
   }
@@ -295,19 +307,6 @@ __device__ __forceinline__ void attn_store_rows(T* row, bool valid, const f32x16
 
 __device__ __forceinline__ unsigned attn_low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// The next tile from `t` on (below `end`) in which a set of rows sees anything; `a`, `b`: two sets of bits of tiles (both count), or null.
-__device__ __forceinline__ int attn_next_tile(int t, int end, const uint64_t* a, const uint64_t* b) {
-  if (!a) return t;
-  while (t < end) {
-    uint64_t w = a[t >> 6];
-    if (b) w |= b[t >> 6];
-    w >>= t & 63;
-    if (w) return min(end, t + (int)__builtin_ctzll(w));
-    t = (t | 63) + 1;
-  }
-  return end;
-}
-
 // The bias of one head by relative position, in LDS: entry x is that of relative position x - span - kAttnPad, clamped, so that a
 // pair of tiles that comes near the clamped ends needs no clamping of its own.
 constexpr int kAttnPad = 96;
@@ -387,16 +386,32 @@ __device__ __forceinline__ void attn_tiles_of_split(const AttnArgs& a, int split
   end = (int)((int64_t)all * (split + 1) / a.splits);
 }
 
-// The tiles in which a panel of 128 rows (two sets of 64) sees anything.
+// The tiles in which a panel of 128 rows (two sets of 64) sees anything, 64 of them at hand at a time.
 struct AttnSeenTiles {
   const uint64_t *a = nullptr, *b = nullptr;
+  uint64_t bits = 0;
+  int group = -1;
   __device__ __forceinline__ AttnSeenTiles(const uint64_t* mask, int64_t at, int64_t tiles, int64_t sets, int first_row) {
     if (!mask) return;
     const int64_t per = (tiles + 63) / 64;
-    a = mask + at + (first_row >> 6) * per;
+    a = b = mask + at + (first_row >> 6) * per;
     if ((first_row >> 6) + 1 < sets) b = a + per;
   }
-  __device__ __forceinline__ int next(int t, int end) const { return attn_next_tile(t, end, a, b); }
+  // the next one from t on, or `end`
+  __device__ __forceinline__ int next(int t, int end) {
+    if (!a) return t;
+    while (t < end) {
+      if (t >> 6 != group) {
+        group = t >> 6;
+        const uint64_t both = a[group] | b[group];
+        bits = (uint64_t)(unsigned)uniform((int)(both >> 32)) << 32 | (unsigned)uniform((int)both);
+      }
+      const uint64_t left = bits >> (t & 63);
+      if (left) return min(end, t + (int)__builtin_ctzll(left));
+      t = (t | 63) + 1;
+    }
+    return end;
+  }
 };
 
 // Which of a tile's 64 positions a row sees, by the mask, and the first `left` of them.
@@ -480,7 +495,7 @@ constexpr float kAttnLeastScale = 1e-37f;
 
 // v where the bit of register r is set (word: shifted by 4 times the half), else `other`.
 __device__ __forceinline__ float attn_select(unsigned word, int r, float v, float other) {
-  const int all = (int)(word << (31 - (8 * (r / 4) + r % 4))) >> 31;
+  const int all = __builtin_amdgcn_sbfe((int)word, 8 * (r / 4) + r % 4, 1);
   const int bits = (all & __builtin_bit_cast(int, v)) | (~all & __builtin_bit_cast(int, other));
   return __builtin_bit_cast(float, bits);
 }

@@ -55,12 +55,14 @@ constexpr int kAttnRowSums = 6;
 // Whether a call needs them, and the weights' part of it.
 template <typename T, bool BIAS> constexpr bool attn_row_sums() { return BIAS || sizeof(T) == 4; }
 
+// (half precision takes sum P as 1; a row of Inf or NaN keeps its weights and its D)
+template <typename T> __device__ __forceinline__ double attn_row_weight(const AttnRowSums& s) {
+  return sizeof(T) == 4 && s.p > 0. && s.p < 1e30 ? 1. / s.p : 1.;
+}
 // What the other kernels take of a row: D, 1 / sum P (single precision) and the sums of dS at the ends.
 template <typename T, bool BIAS>
 __device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat, float delta, const AttnRowSums& s) {
-  // (half precision takes sum P as 1; a row of Inf or NaN keeps its D)
-  const bool usable = s.p > 0. && s.p < 1e30;
-  const double weight = sizeof(T) == 4 && usable ? 1. / s.p : 1., more = s.ds * weight;
+  const double weight = attn_row_weight<T>(s), more = s.ds * weight;
   a.delta[flat] = more == more ? (float)(delta + more) : delta;
   if constexpr (sizeof(T) == 4) a.weight[flat] = (float)weight;
   if constexpr (BIAS) {
@@ -68,17 +70,15 @@ __device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat,
     a.ends[2 * flat + 1] = (float)(weight * (s.high - more * s.high_p));
   }
 }
-template <typename T, bool BIAS>
-__global__ __launch_bounds__(256) void attention_rows_kernel(const AttnArgs a) {
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m, flat = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (flat >= rows) return;
+template <bool BIAS> __device__ __forceinline__ AttnRowSums attn_row_sums_of(const AttnArgs& a, int64_t flat, bool ends) {
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   AttnRowSums s = {};
   for (int i = 0; i < a.splits; ++i) {
     const double* from = a.row_sums + (i * rows + flat) * kAttnRowSums;
     s.ds += from[0], s.p += from[1];
-    if (BIAS) s.low += from[2], s.low_p += from[3], s.high += from[4], s.high_p += from[5];
+    if (BIAS && ends) s.low += from[2], s.low_p += from[3], s.high += from[4], s.high_p += from[5];
   }
-  attn_finish_row<T, BIAS>(a, flat, a.delta[flat], s);
+  return s;
 }
 
 // A workgroup's panel of queries for the backward pass.
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   delta = attn_sum_halves(delta);
 
   const MaskLayout lay(a.m, a.k);
-  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
+  AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   int position = 0;
   if (BIAS) {
     attn_fill_bias<T>(lds_bias, a, head, tid, 256);
@@ -172,11 +172,13 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   f32x16 acc[D / 32] = {};
   AttnScale ds_scale;
   typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  const auto whole_k = stage_k.whole_offsets(a.k16s.row, tid);
+  const auto whole_v = stage_v.whole_offsets(a.v16s.row, tid);
   uint64_t word_next = 0;
   auto load = [&](int t) {
     word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
-    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
-    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, whole_k, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, whole_v, tid);
   };
   int t = tiles.next(begin, end);
   if (t < end) load(t);
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     for (int i = 0; i < kAttnRowSums; ++i) s[i] += __shfl_xor(s[i], 32);
     const AttnRowSums all = {s[0], s[1], s[2], s[3], s[4], s[5]};
     if (a.splits == 1) {
-      if (sizeof(T) == 4 && all.p > 0. && all.p < 1e30) weight = (float)(1. / all.p);
+      weight = (float)attn_row_weight<T>(all);
       if (valid && half == 0) attn_finish_row<T, BIAS>(a, own.flat, delta, all);
     } else if (valid && half == 0) {
       if (at.split == 0) a.delta[own.flat] = delta;
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     attn_store_rows<float, D>(a.part + (at.split * rows + own.flat) * a.d, valid, acc, factor, a.d, half);
   }
 }
-// Runs before attention_rows_kernel: parts are sums of P as lse gives it, with D as it is then.
+// Runs before the parts are added up: they are sums of P as lse gives it, with D as it is then.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_dq_again_kernel(const AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -298,34 +300,30 @@ __global__ __launch_bounds__(256) void attention_dq_again_kernel(const AttnArgs 
   }
 }
 
-// Sums of dS by relative position, a wave's own: x holds keys in its registers and queries in its lanes.  The block of 32 x 32 goes
-// through LDS, and lane l sums the l-th diagonal.  Each relative position between the clamped ends then has one lane that adds it.
-__device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block, float* sums, int near, int span, double& low,
-                                                   double& high, int lane) {
-  const int half = lane >> 5;
+// Sums of dS by relative position, a wave's own: x holds keys in its registers and queries in its lanes.  The block of 32 x 32 goes through
+// LDS by diagonals: key j and query i at row j - i + 31 and column i of 63 rows, whose other places stay 0, and lane l adds up row l.  Each
+// relative position between the clamped ends then has one lane that adds it.
+constexpr int kAttnDiagonalPitch = 36, kAttnDiagonalBlock = 63 * kAttnDiagonalPitch;      // floats per wave
+__device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block, float* sums, int near, int span, double& low, double& high, int lane) {
+  float* at = block + (4 * (lane >> 5) - (lane & 31) + 31) * kAttnDiagonalPitch + (lane & 31);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int r = 0; r < 16; ++r) block[(lane & 31) * 33 + 8 * (r / 4) + 4 * half + r % 4] = x[r];
+  for (int r = 0; r < 16; ++r) at[(8 * (r / 4) + r % 4) * kAttnDiagonalPitch] = x[r];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const int off = lane - 31;                              // key minus query within the block
-  float s = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < 32; ++i) {
-    const int j = i + off;
-    const float v = block[i * 33 + min(max(j, 0), 31)];
-    s += j >= 0 && j < 32 ? v : 0.f;
-  }
-  const int rel = near + off;
+  const float* row = block + min(lane, 62) * kAttnDiagonalPitch;
+  f32x4 s = {};
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) s += *reinterpret_cast<const f32x4*>(row + i);
+  const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+  const int rel = near + lane - 31;                       // of row `lane`
   if (lane < 63) {
-    if (rel <= -span) low += s;
-    else if (rel >= span) high += s;
-    else sums[rel + span] += s;
+    if (rel <= -span) low += sum;
+    else if (rel >= span) high += sum;
+    else sums[rel + span] += sum;
   }
 }
-
-constexpr int kAttnDiagonalBlock = 32 * 33;               // floats per wave
 
 // The gradient of the bias by relative position, by panels of 128 queries: the blocks near the diagonal are formed again, with the
 // right D; what lies at the ends of the bias attention_dq_kernel has summed by rows.
@@ -335,7 +333,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
-  float* lds_blocks = lds_bias + attn_bias_entries(a.span);
+  float* lds_blocks = lds_bias + (attn_bias_entries(a.span) + 3) / 4 * 4;
   float* lds_sums = lds_blocks + kAttnWaves * kAttnDiagonalBlock;
   const int n = 2 * a.span + 1;
 
@@ -358,7 +356,9 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   own.load(a, at, f, row, valid, half);
   attn_fill_bias<T>(lds_bias, a, head, tid, 256);
   float* sums = lds_sums + wave * n;
+  float* block = lds_blocks + wave * kAttnDiagonalBlock;
   for (int x = lane; x < n; x += 64) sums[x] = 0.f;
+  for (int x = lane; x < kAttnDiagonalBlock; x += 64) block[x] = 0.f;
 
   float delta = 0.f, weight = 1.f;
   double low = 0., high = 0.;
@@ -369,13 +369,15 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   }
 
   const MaskLayout lay(a.m, a.k);
-  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
+  AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   typename Tile::template Stage<kAttnTile, 256> stage_k, stage_v;
+  const auto whole_k = stage_k.whole_offsets(a.k16s.row, tid);
+  const auto whole_v = stage_v.whole_offsets(a.v16s.row, tid);
   uint64_t word_next = 0;
   auto load = [&](int t) {
     word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
-    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
-    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, whole_k, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, whole_v, tid);
   };
   int t = tiles.next(begin, end);
   if (t < end) load(t);
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r] * weight * __builtin_fmaf(y[r], own.to_dp, -delta), 0.f);
-      attn_sum_diagonals(x, lds_blocks + wave * kAttnDiagonalBlock, sums, near, a.span, low, high, lane);
+      attn_sum_diagonals(x, block, sums, near, a.span, low, high, lane);
     }
   }
 #pragma unroll
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   const float scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale), to_dp = f.g * f.v, c = scale * kLog2e;
 
   const MaskLayout lay(a.m, a.k);
-  const AttnSeenTiles seen_tiles(a.mask, lay.col_tiles, lay.ti, lay.tj, first_key);
+  AttnSeenTiles seen_tiles(a.mask, lay.col_tiles, lay.ti, lay.tj, first_key);
   const int position = BIAS ? attn_position(a, batch) : 0;
 
   // the next (head of the group, tile of queries) that the panel takes part in
@@ -478,12 +480,14 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   AttnScale ds_scale;
   typename Tile::template Stage<kAttnTile, 256> stage_q, stage_g;
   float stat = 0.f;
+  const auto whole_q = stage_q.whole_offsets(a.q16s.row, tid);
+  const auto whole_g = stage_g.whole_offsets(a.g16s.row, tid);
   uint64_t word_next = 0;
   auto load = [&](int64_t at) {
     const int h = (int)(at / tiles), t = (int)(at - (int64_t)h * tiles), rows = a.m - t * kAttnTile;
     word_next = attn_word(a.mask ? a.mask + lay.col_words + (int64_t)t * lay.tj * 64 : nullptr, key, valid);
-    stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, tid);
-    stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, tid);
+    stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, whole_q, tid);
+    stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, whole_g, tid);
     const int r = tid & 63;
     if (tid < (kTerms == 2 ? 192 : 128))
       stat = r < rows ? (tid < 64 ? a.lse : tid < 128 ? a.delta : a.weight)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
@@ -613,59 +617,76 @@ __global__ __launch_bounds__(256) void attention_dkv_again_kernel(const AttnArgs
 }
 
 // Adds up what `splits` workgroups left of each of the rows, in their order: of one array, or of two that lie one behind the other; a
-// thread has four neighbouring elements of a row.  weight: what a row is taken times, or null.
+// thread has four neighbouring elements of a row.
 struct AttnSum { AttnStrides to; void* out; };
 template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part,
-                                                            const float* weight, AttnSum first, AttnSum second) {
-  const int pieces = (d + 3) / 4;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = rows * pieces;
-  const bool behind = at >= all;
-  if (behind) part += splits * rows * d;
-  const AttnSum& x = behind ? second : first;
-  if (at >= 2 * all || !x.out) return;
-  const int64_t flat = (behind ? at - all : at) / pieces;
-  const int c = (int)((behind ? at - all : at) - flat * pieces) * 4;
+__device__ __forceinline__ void attn_add_parts(int splits, int64_t rows, int heads, int per_head, int d, const float* part, int64_t flat, int c, float weight,
+                                               const AttnSum& x) {
   f32x4 s = {};
 #pragma unroll 4
   for (int i = 0; i < splits; ++i) s += attn_load_piece<float>(part + (i * rows + flat) * d, c, d);
-  if (weight) s *= weight[flat];
+  s *= weight;
   const int64_t bh = flat / per_head;
   T* row = static_cast<T*>(x.out) + bh / heads * x.to.batch + bh % heads * x.to.head + (flat % per_head) * x.to.row;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (c + e < d) row[c + e] = (T)s[e];
 }
+template <typename T>
+__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part, AttnSum first,
+                                                            AttnSum second) {
+  const int pieces = (d + 3) / 4;
+  int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t all = rows * pieces;
+  if (at >= 2 * all) return;
+  const bool behind = at >= all;
+  if (behind) at -= all;
+  attn_add_parts<T>(splits, rows, heads, per_head, d, part + (behind ? splits * rows * d : 0), at / pieces, (int)(at % pieces) * 4, 1.f, behind ? second : first);
+}
+// The same for dQ, whose rows' sums over their keys are added up and put to use here (SUMS).
+template <typename T, bool BIAS, bool SUMS>
+__global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a) {
+  const int pieces = (a.d + 3) / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.batch * a.heads * a.m;
+  if (at >= rows * pieces) return;
+  const int64_t flat = at / pieces;
+  const bool first = at % pieces == 0;
+  float weight = 1.f;
+  if (SUMS && (sizeof(T) == 4 || first)) {
+    const AttnRowSums s = attn_row_sums_of<BIAS>(a, flat, first);
+    weight = (float)attn_row_weight<T>(s);
+    if (first) attn_finish_row<T, BIAS>(a, flat, a.delta[flat], s);
+  }
+  attn_add_parts<T>(a.splits, rows, a.heads, a.m, a.d, a.part, flat, (int)(at % pieces) * 4, weight, AttnSum{a.dq, a.dQ});
+}
 
-// dtable of one head: the panels' sums by relative position (sixteen waves take panels in turn, then are added up in their order), then
-// those of a bucket, in ascending position.
+// dtable of one head: the panels' sums by relative position (runs of panels by as many groups of threads as 1024 allow, added up in their
+// order), then those of a bucket, in ascending position, eight threads to a bucket.
 template <typename T>
 __global__ __launch_bounds__(1024) void attention_dtable_kernel(const AttnArgs a, int parts, T* dtable) {
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  double* sums = reinterpret_cast<double*>(lds_raw);
-  int* buckets = reinterpret_cast<int*>(sums + 2 * a.span + 1);
-  __shared__ double waves[16][64];
-  const int n = 2 * a.span + 1, head = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = 2 * a.span + 1, head = blockIdx.x, groups = n < 1024 ? 1024 / n : 1;
+  double* sums = reinterpret_cast<double*>(lds_raw);      // [groups][n], then [n] in the first
+  int* buckets = reinterpret_cast<int*>(sums + groups * n);
   const float* from = a.part_bias + (int64_t)head * parts * n;
-  for (int x0 = 0; x0 < n; x0 += 64) {
-    const int x = min(x0 + lane, n - 1);
+  for (int at = threadIdx.x; at < groups * n; at += 1024) {
+    const int group = at / n, x = at - group * n, end = (int)((int64_t)parts * (group + 1) / groups);
     double s = 0.;
-#pragma unroll 4
-    for (int i = wave; i < parts; i += 16) s += from[(int64_t)i * n + x];
-    waves[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && x0 + lane < n) {
-      double all = 0.;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) all += waves[w][lane];
-      sums[x] = all;
-      buckets[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
-    }
-    __syncthreads();
+#pragma unroll 8
+    for (int i = (int)((int64_t)parts * group / groups); i < end; ++i) s += from[(int64_t)i * n + x];
+    sums[at] = s;
+    if (group == 0) buckets[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
   }
-  // eight threads to a bucket, each an eighth of the positions
+  __syncthreads();
+  for (int x = threadIdx.x; x < n; x += 1024) {
+    double s = sums[x];
+    for (int g = 1; g < groups; ++g) s += sums[g * n + x];
+    sums[x] = s;
+  }
+  __syncthreads();
   const int b = threadIdx.x >> 3, eighth = threadIdx.x & 7;
   double s = 0.;
+#pragma unroll 4
   for (int x = n * eighth / 8; x < n * (eighth + 1) / 8; ++x) s += buckets[x] == b ? sums[x] : 0.;
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);

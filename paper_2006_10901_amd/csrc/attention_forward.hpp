@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   const float scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
 
   const MaskLayout lay(a.m, a.k);
-  const AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
+  AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   int position = 0;
   if (BIAS) {
     attn_fill_bias<T>(lds_bias, a, head, tid, 256);
@@ -43,11 +43,13 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
   AttnRunning run;
   typename Tile::template Stage<kAttnTile, 256> stage_k;
   typename Tile::template Stage<kAttnTile, 256, Tile::kPitchT> stage_v;
+  const auto whole_k = stage_k.whole_offsets(a.k16s.row, tid);
+  const auto whole_v = stage_v.whole_offsets(a.v16s.row, tid);
   uint64_t word_next = 0;
   auto load = [&](int t) {
     word_next = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)t * lay.ti * 64 : nullptr, row, valid);
-    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, tid);
-    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, tid);
+    stage_k.load(K + (int64_t)t * kAttnTile * a.k16s.row, a.k16s.row, seen - t * kAttnTile, a.width, whole_k, tid);
+    stage_v.load(V + (int64_t)t * kAttnTile * a.v16s.row, a.v16s.row, seen - t * kAttnTile, a.width, whole_v, tid);
   };
   int t = tiles.next(begin, end);
   if (t < end) load(t);
