@@ -445,9 +445,10 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   const int first_key = panel * kAttnPanel, wave_key = first_key + wave * 32, key = wave_key + (lane & 31);
   const bool valid = key < seen;
   const int tiles = (a.m + kAttnTile - 1) / kAttnTile;
-  // the tiles of all heads of the group, one after the other, are dealt to the splits in runs
-  const int64_t all = (int64_t)a.group * tiles;
-  const int64_t begin = first_key < seen ? all * split / a.splits : 0, end = first_key < seen ? all * (split + 1) / a.splits : 0;
+  // the tiles of all heads of the group, one after the other, are dealt to the splits in runs: from tile t of head h on, up to that of `last`
+  const int64_t all = first_key < seen ? (int64_t)a.group * tiles : 0, begin = all * split / a.splits, end = all * (split + 1) / a.splits;
+  int h = tiles ? (int)(begin / tiles) : 0, t = (int)(begin - (int64_t)h * tiles);
+  const int last_h = tiles ? (int)(end / tiles) : 0, last_t = (int)(end - (int64_t)last_h * tiles);
 
   const _Float16* Q = a.q16 + batch * a.q16s.batch + (int64_t)kv_head * a.group * a.q16s.head;
   const _Float16* dO = a.g16 + batch * a.g16s.batch + (int64_t)kv_head * a.group * a.g16s.head;
@@ -464,16 +465,16 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   AttnSeenTiles seen_tiles(a.mask, lay.col_tiles, lay.ti, lay.tj, first_key);
   const int position = BIAS ? attn_position(a, batch) : 0;
 
-  // the next (head of the group, tile of queries) that the panel takes part in
-  auto next = [&](int64_t at) {
-    while (at < end) {
-      const int h = (int)(at / tiles), t = (int)(at - (int64_t)h * tiles);
-      const int stop = (int)min((int64_t)tiles, end - (int64_t)h * tiles);
-      const int n = seen_tiles.next(t, stop);
-      if (n < stop) return (int64_t)h * tiles + n;
-      at = (int64_t)h * tiles + stop;
+  // from there on the next that the panel takes part in; whether there is one
+  auto next = [&]() {
+    while (h < last_h || (h == last_h && t < last_t)) {
+      const int stop = h == last_h ? last_t : tiles;
+      t = seen_tiles.next(t, stop);
+      if (t < stop) return true;
+      ++h;
+      t = 0;
     }
-    return end;
+    return false;
   };
 
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
@@ -483,8 +484,8 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
   const auto whole_q = stage_q.whole_offsets(a.q16s.row, tid);
   const auto whole_g = stage_g.whole_offsets(a.g16s.row, tid);
   uint64_t word_next = 0;
-  auto load = [&](int64_t at) {
-    const int h = (int)(at / tiles), t = (int)(at - (int64_t)h * tiles), rows = a.m - t * kAttnTile;
+  auto load = [&]() {
+    const int rows = a.m - t * kAttnTile;
     word_next = attn_word(a.mask ? a.mask + lay.col_words + (int64_t)t * lay.tj * 64 : nullptr, key, valid);
     stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, whole_q, tid);
     stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, whole_g, tid);
@@ -492,11 +493,11 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
     if (tid < (kTerms == 2 ? 192 : 128))
       stat = r < rows ? (tid < 64 ? a.lse : tid < 128 ? a.delta : a.weight)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
   };
-  int64_t at = next(begin);
+  bool more = next();
   int bias_head = -1;
   float low = 0.f, high = 0.f;                            // the bias at its ends
-  if (at < end) load(at);
-  for (int set = 0; at < end; set ^= Tile::kSets - 1) {
+  if (more) load();
+  for (int set = 0; more; set ^= Tile::kSets - 1) {
     char* lds_q = lds_raw + set * Tile::kPair;
     char* lds_g = lds_q + kAttnTile * Tile::kPitch;
     float* lds_lse = lds_stats + set * 5 * kAttnTile;
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
     if (Tile::kSets == 1) __syncthreads();
     stage_q.store(lds_q, tid);
     stage_g.store(lds_g, tid);
-    const int h = (int)(at / tiles), row0 = (int)(at - (int64_t)h * tiles) * kAttnTile;
+    const int row0 = t * kAttnTile;
     const uint64_t word = valid ? word_next : 0ull;
     if (BIAS && h != bias_head) {
       __syncthreads();                                    // the head before may still be at work
@@ -527,8 +528,9 @@ __global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1)
       lds_lse[tid] = stat;
     }
     __syncthreads();
-    at = next(at + 1);
-    if (at < end) load(at);
+    ++t;
+    more = next();
+    if (more) load();
     if (!__any(word != 0)) continue;
     const bool hide = __any(word != ~0ull);
 #pragma unroll
