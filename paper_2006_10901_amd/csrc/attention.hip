@@ -259,15 +259,21 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
       attention_sum_dq_kernel<T, BIAS, attn_row_sums<T, BIAS>()><<<dim3((unsigned)up(x.rows * pieces, 256)), dim3(256), 0, stream>>>(a);
       if (hipGetLastError() != hipSuccess) return false;
     }
-    if (BIAS && a.part_bias) {
-      a.splits = x.dbias_splits;
-      const int lds = kTiles + bias + 16 + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
-      if (!launch(attention_dbias_kernel<T, D>, x.dq_blocks * a.splits, lds, a, stream)) return false;
-    }
+  }
+  // dK and dV, and in the same launch the sums for the bias, unless the LDS that those take would leave fewer workgroups to a compute unit
+  a.splits = x.dkv_splits, a.bias_splits = x.dbias_splits;
+  const int64_t blocks = x.dkv_blocks * a.splits, bias_blocks = BIAS && a.part_bias ? x.dq_blocks * a.bias_splits : 0;
+  const int lds = kTiles + Tile::kSets * 5 * kAttnTile * 4 + bias, bias_lds = Tile::kPair + bias + 16 + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
+  const bool together = bias_blocks > 0 && std::max(lds, bias_lds) * attn_dkv_each<T, D>() <= 160 * 1024;
+  a.bias_from = (int)blocks;
+  if (blocks + (together ? bias_blocks : 0) > 0 &&
+      !launch(attention_dkv_kernel<T, D, BIAS>, blocks + (together ? bias_blocks : 0), together ? std::max(lds, bias_lds) : lds, a, stream))
+    return false;
+  if (bias_blocks > 0 && !together) {
+    a.bias_from = 0;
+    if (!launch(attention_dkv_kernel<T, D, BIAS>, bias_blocks, bias_lds, a, stream)) return false;
   }
   if (x.dkv_blocks > 0) {
-    a.splits = x.dkv_splits;
-    if (!launch(attention_dkv_kernel<T, D, BIAS>, x.dkv_blocks * a.splits, kTiles + Tile::kSets * 5 * kAttnTile * 4 + bias, a, stream)) return false;
     if (a.mask && !launch(attention_dkv_again_kernel<T>, x.dkv_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
       attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(

@@ -61,6 +61,7 @@ struct AttnArgs {
   double* row_sums;      // workspace: of every split and row, the sums over its keys
   unsigned* again;       // workspace, with a mask: of each wave of a panel kernel, which of its rows are not finite
   float* part_bias;      // workspace: sums of dS by relative position, one set of 2 span + 1 per panel
+  int bias_from, bias_splits;   // from which workgroup of attention_dkv_kernel on they make those sums, and over how many a panel is split
 };
 
 // The sparse matrix as bits, in words of 64: for every tile of 64 columns a word per row (row_words), for every tile of 64 rows a word
@@ -339,8 +340,9 @@ __device__ __forceinline__ int attn_seen(const AttnArgs& a, int batch) { return 
 // heads, 512 queries, fp16: MEASURED.)
 struct AttnPlace {
   int batch, kv_head, piece;
-  __device__ __forceinline__ AttnPlace(const AttnArgs& a, int inner) {
-    const int id = blockIdx.x, total = gridDim.x, xcd = id & 7;
+  __device__ __forceinline__ AttnPlace(const AttnArgs& a, int inner) : AttnPlace(a, inner, blockIdx.x, gridDim.x) {}
+  __device__ __forceinline__ AttnPlace(const AttnArgs& a, int inner, int id, int total) {
+    const int xcd = id & 7;
     if (!a.by_length) {
       const int each = total >> 3, rest = total & 7;
       int work = xcd * each + min(xcd, rest) + (id >> 3);
@@ -370,12 +372,13 @@ struct AttnPlace {
 // The panel of 128 queries that a workgroup works on, and which part of the keys.
 struct AttnPanelOf {
   int split, panel, batch, kv_head, head, panels;
-  __device__ __forceinline__ AttnPanelOf(const AttnArgs& a, int rows) {
+  __device__ __forceinline__ AttnPanelOf(const AttnArgs& a, int rows) : AttnPanelOf(a, rows, a.splits, blockIdx.x, gridDim.x) {}
+  __device__ __forceinline__ AttnPanelOf(const AttnArgs& a, int rows, int splits, int id, int total) {
     panels = (rows + kAttnPanel - 1) / kAttnPanel;
-    const AttnPlace at(a, a.group * panels * a.splits);
+    const AttnPlace at(a, a.group * panels * splits, id, total);
     batch = at.batch, kv_head = at.kv_head;
-    split = at.piece % a.splits;
-    const int rest = at.piece / a.splits;
+    split = at.piece % splits;
+    const int rest = at.piece / splits;
     panel = rest % panels;
     head = kv_head * a.group + rest / panels;
   }

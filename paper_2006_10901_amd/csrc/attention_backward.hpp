@@ -328,17 +328,16 @@ __device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block
 // The gradient of the bias by relative position, by panels of 128 queries: the blocks near the diagonal are formed again, with the
 // right D; what lies at the ends of the bias attention_dq_kernel has summed by rows.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) {
+__device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
-  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
+  float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kPair);
   float* lds_blocks = lds_bias + (attn_bias_entries(a.span) + 3) / 4 * 4;
   float* lds_sums = lds_blocks + kAttnWaves * kAttnDiagonalBlock;
   const int n = 2 * a.span + 1;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
-  const AttnPanelOf at(a, a.m);
+  const AttnPanelOf at(a, a.m, a.bias_splits, blockIdx.x - a.bias_from, gridDim.x - a.bias_from);
   const int batch = at.batch, head = at.head, kv_head = at.kv_head;
   const int seen = attn_seen(a, batch);
   const int first_row = at.panel * kAttnPanel, wave_row = first_row + wave * 32, row = wave_row + (lane & 31);
@@ -347,7 +346,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   // tiles that hold relative positions between the ends
   const int lowest = position + first_row - a.span - kAttnTile, highest = position + first_row + kAttnPanel + a.span;
   const int from = max(lowest, 0) / kAttnTile, to = max(from, min((seen + kAttnTile - 1) / kAttnTile, max(highest, 0) / kAttnTile + 1));
-  const int begin = from + (to - from) * at.split / a.splits, end = from + (to - from) * (at.split + 1) / a.splits;
+  const int begin = from + (to - from) * at.split / a.bias_splits, end = from + (to - from) * (at.split + 1) / a.bias_splits;
 
   const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
   const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
@@ -381,10 +380,10 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
   };
   int t = tiles.next(begin, end);
   if (t < end) load(t);
-  for (int set = 0; t < end; set ^= Tile::kSets - 1) {
-    char* lds_k = lds_raw + set * Tile::kPair;
+  while (t < end) {
+    char* lds_k = lds_raw;
     char* lds_v = lds_k + kAttnTile * Tile::kPitch;
-    if (Tile::kSets == 1) __syncthreads();
+    __syncthreads();
     stage_k.store(lds_k, tid);
     stage_v.store(lds_v, tid);
     const int key0 = t * kAttnTile;
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
     sums[2 * a.span] += (float)high;
   }
   __syncthreads();
-  float* sum_to = a.part_bias + ((((int64_t)head * a.batch + batch) * at.panels + at.panel) * a.splits + at.split) * n;
+  float* sum_to = a.part_bias + ((((int64_t)head * a.batch + batch) * at.panels + at.panel) * a.bias_splits + at.split) * n;
   for (int x = tid; x < n; x += 256) {
     float s = 0.f;
 #pragma unroll
@@ -427,18 +426,23 @@ __global__ __launch_bounds__(256) void attention_dbias_kernel(const AttnArgs a) 
 
 // dK and dV, by panels of 128 keys: a wave has 32 of them, tiles of 64 queries, of every head that shares the keys, are shared by the waves.
 // Two workgroups to a compute unit as for dQ (fp32, 64 columns 369 -> 292 us, fp16 96 106 -> 98), but not at 128 columns (fp16 143 -> 235).
+template <typename T, int D> constexpr int attn_dkv_each() { return D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1; }
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1) void attention_dkv_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, (attn_dkv_each<T, D>())) void attention_dkv_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  if (BIAS && (int)blockIdx.x >= a.bias_from) {
+    attn_dbias<T, D>(a, lds_raw);
+    return;
+  }
   float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set, 64 times: lse (as an exponent of 2; with
   // a bias lse itself, and the exponents with the bias's two ends), D, what P is taken times
   float* lds_bias = lds_stats + Tile::kSets * 5 * kAttnTile;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
   const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
-  const AttnPlace place(a, panels * a.splits);
+  const AttnPlace place(a, panels * a.splits, blockIdx.x, BIAS ? a.bias_from : gridDim.x);
   const int split = place.piece % a.splits, panel = place.piece / a.splits, batch = place.batch, kv_head = place.kv_head;
 
   const int seen = attn_seen(a, batch);
