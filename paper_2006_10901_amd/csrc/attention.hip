@@ -243,12 +243,12 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
 }
 
 template <typename T, int D, bool BIAS>
-bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
+bool launch_backward(const Plan& x, AttnArgs a, char* w, void* dtable, hipStream_t stream) {
   using Tile = AttnTile<D, attn_terms<T>()>;
   constexpr int kTiles = Tile::kSets * Tile::kPair;
   const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
   const int64_t pieces = up(a.d, 4);
-  float* part = a.part = reinterpret_cast<float*>(w + x.part);
+  a.part = reinterpret_cast<float*>(w + x.part);
   a.again = reinterpret_cast<unsigned*>(w + x.backward_again);
   if ((x.dq_blocks > 0 || x.dkv_blocks > 0) && !prepare_operands<T, D>(x, a, w, true, stream)) return false;
   if (x.dq_blocks > 0) {
@@ -273,15 +273,13 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
     a.bias_from = 0;
     if (!launch(attention_dkv_kernel<T, D, BIAS>, bias_blocks, bias_lds, a, stream)) return false;
   }
-  if (x.dkv_blocks > 0) {
-    if (a.mask && !launch(attention_dkv_again_kernel<T>, x.dkv_blocks * a.splits, 0, a, stream)) return false;
-    if (a.splits > 1) {
-      attention_sum_kernel<T><<<dim3((unsigned)up(2 * x.kv_rows * pieces, 256)), dim3(256), 0, stream>>>(
-          a.splits, x.kv_rows, a.kv_heads, a.k, a.d, part, AttnSum{a.dk, a.dK}, AttnSum{a.dv, a.dV});
-      if (hipGetLastError() != hipSuccess) return false;
-    }
-  }
-  return true;
+  if (x.dkv_blocks > 0 && a.mask && !launch(attention_dkv_again_kernel<T>, x.dkv_blocks * a.splits, 0, a, stream)) return false;
+  const int tables = dtable ? a.heads : 0, n = 2 * a.span + 1;
+  const int64_t sums = a.splits > 1 ? up(2 * x.kv_rows * pieces, 1024) : 0;
+  if (tables + sums == 0) return true;
+  attention_finish_kernel<T><<<dim3((unsigned)(tables + sums)), dim3(1024), tables ? (n < 1024 ? 1024 / n : 1) * n * 8 + n * 4 : 0, stream>>>(
+      a, tables, (int)x.parts, static_cast<T*>(dtable));
+  return hipGetLastError() == hipSuccess;
 }
 
 template <typename T, bool BIAS>
@@ -293,11 +291,11 @@ bool dispatch_forward(const Plan& x, const AttnArgs& a, char* w, hipStream_t str
 }
 
 template <typename T, bool BIAS>
-bool dispatch_backward(const Plan& x, const AttnArgs& a, char* w, hipStream_t stream) {
-  if (a.d <= 32) return launch_backward<T, 32, BIAS>(x, a, w, stream);
-  if (a.d <= 64) return launch_backward<T, 64, BIAS>(x, a, w, stream);
-  if (a.d <= 96) return launch_backward<T, 96, BIAS>(x, a, w, stream);
-  return launch_backward<T, 128, BIAS>(x, a, w, stream);
+bool dispatch_backward(const Plan& x, const AttnArgs& a, char* w, void* dtable, hipStream_t stream) {
+  if (a.d <= 32) return launch_backward<T, 32, BIAS>(x, a, w, dtable, stream);
+  if (a.d <= 64) return launch_backward<T, 64, BIAS>(x, a, w, dtable, stream);
+  if (a.d <= 96) return launch_backward<T, 96, BIAS>(x, a, w, dtable, stream);
+  return launch_backward<T, 128, BIAS>(x, a, w, dtable, stream);
 }
 
 inline bool workspace_ok(const void* workspace, int64_t bytes, int64_t needed) {
@@ -360,12 +358,7 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   a.part_bias = dtable ? reinterpret_cast<float*>(w + x.part_bias) : nullptr;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (!(table ? dispatch_backward<T, true>(x, a, w, s) : dispatch_backward<T, false>(x, a, w, s))) return SPDL_ERR_LAUNCH;
-  if (dtable) {
-    const int n = 2 * p->span + 1;
-    attention_dtable_kernel<T><<<dim3((unsigned)p->heads), dim3(1024), (n < 1024 ? 1024 / n : 1) * n * 8 + n * 4, s>>>(a, (int)x.parts, static_cast<T*>(dtable));
-    if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
-  }
+  if (!(table ? dispatch_backward<T, true>(x, a, w, dtable, s) : dispatch_backward<T, false>(x, a, w, dtable, s))) return SPDL_ERR_LAUNCH;
   return SPDL_OK;
 }
 

@@ -638,18 +638,7 @@ __device__ __forceinline__ void attn_add_parts(int splits, int64_t rows, int hea
   for (int e = 0; e < 4; ++e)
     if (c + e < d) row[c + e] = (T)s[e];
 }
-template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(int splits, int64_t rows, int heads, int per_head, int d, const float* part, AttnSum first,
-                                                            AttnSum second) {
-  const int pieces = (d + 3) / 4;
-  int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t all = rows * pieces;
-  if (at >= 2 * all) return;
-  const bool behind = at >= all;
-  if (behind) at -= all;
-  attn_add_parts<T>(splits, rows, heads, per_head, d, part + (behind ? splits * rows * d : 0), at / pieces, (int)(at % pieces) * 4, 1.f, behind ? second : first);
-}
-// The same for dQ, whose rows' sums over their keys are added up and put to use here (SUMS).
+// Of dQ, whose rows' sums over their keys are added up and put to use here (SUMS).
 template <typename T, bool BIAS, bool SUMS>
 __global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a) {
   const int pieces = (a.d + 3) / 4;
@@ -669,19 +658,19 @@ __global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a)
 // dtable of one head: the panels' sums by relative position (runs of panels by as many groups of threads as 1024 allow, added up in their
 // order), then those of a bucket, in ascending position, eight threads to a bucket.
 template <typename T>
-__global__ __launch_bounds__(1024) void attention_dtable_kernel(const AttnArgs a, int parts, T* dtable) {
-  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  const int n = 2 * a.span + 1, head = blockIdx.x, groups = n < 1024 ? 1024 / n : 1;
+__device__ __forceinline__ void attn_dtable(const AttnArgs& a, int head, int parts, T* dtable, char* lds_raw) {
+  const int n = 2 * a.span + 1, groups = n < 1024 ? 1024 / n : 1;
   double* sums = reinterpret_cast<double*>(lds_raw);      // [groups][n], then [n] in the first
   int* buckets = reinterpret_cast<int*>(sums + groups * n);
   const float* from = a.part_bias + (int64_t)head * parts * n;
   for (int at = threadIdx.x; at < groups * n; at += 1024) {
     const int group = at / n, x = at - group * n, end = (int)((int64_t)parts * (group + 1) / groups);
+    const int bucket = a.bucket_of[x];
     double s = 0.;
-#pragma unroll 8
+#pragma unroll 16
     for (int i = (int)((int64_t)parts * group / groups); i < end; ++i) s += from[(int64_t)i * n + x];
     sums[at] = s;
-    if (group == 0) buckets[x] = min(max(a.bucket_of[x], 0), a.buckets - 1);
+    if (group == 0) buckets[x] = min(max(bucket, 0), a.buckets - 1);
   }
   __syncthreads();
   for (int x = threadIdx.x; x < n; x += 1024) {
@@ -697,6 +686,24 @@ __global__ __launch_bounds__(1024) void attention_dtable_kernel(const AttnArgs a
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
   if (eighth == 0 && b < a.buckets) dtable[(int64_t)head * a.buckets + b] = (T)s;
+}
+
+// What is left when the panels are done: dtable, a workgroup per head (`tables` of them), and dK and dV added up where they were split.
+template <typename T>
+__global__ __launch_bounds__(1024) void attention_finish_kernel(const AttnArgs a, int tables, int parts, T* dtable) {
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  if ((int)blockIdx.x < tables) {
+    attn_dtable<T>(a, blockIdx.x, parts, dtable, lds_raw);
+    return;
+  }
+  const int pieces = (a.d + 3) / 4;
+  const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k, all = rows * pieces;
+  int64_t at = (int64_t)(blockIdx.x - tables) * 1024 + threadIdx.x;
+  if (at >= 2 * all) return;
+  const bool behind = at >= all;
+  if (behind) at -= all;
+  attn_add_parts<T>(a.splits, rows, a.kv_heads, a.k, a.d, a.part + (behind ? a.splits * rows * a.d : 0), at / pieces, (int)(at % pieces) * 4, 1.f,
+                    behind ? AttnSum{a.dv, a.dV} : AttnSum{a.dk, a.dK});
 }
 
 }  // namespace spdl
