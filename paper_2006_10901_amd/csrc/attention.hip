@@ -79,7 +79,9 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   // tiles near the diagonal that a panel meets
   x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 1, 3);
   x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dbias_splits;
-  x.most_parts = (int)std::min<int64_t>(64, std::max<int64_t>(1, up(std::max<int64_t>(group * p.m, p.k), 64)));
+  // workgroups that look for the largest number of a head: of 64 rows at least, and no more of them in all than 2^16 for each operand
+  const int64_t kv = std::max<int64_t>((int64_t)p.batch * p.kv_heads, 1);
+  x.most_parts = (int)std::max<int64_t>(1, std::min<int64_t>({64, up(std::max<int64_t>(group * p.m, p.k), 64), (1 << 16) / kv}));
 
   int64_t terms = 0, end = 0;
   const int64_t longest = std::max(std::max(p.Q.row, p.K.row), std::max(p.V.row, p.dO.row));
@@ -136,10 +138,9 @@ bool sizes_ok(const spdl_attention_problem& p) {
   if (p.heads > 0 && (p.kv_heads < 1 || p.heads % p.kv_heads)) return false;
   if (p.span < 0 || p.span > kAttnSpanMax || p.buckets < 0 || p.buckets > kAttnBucketsMax) return false;
   if (!std::isfinite(p.scale)) return false;
-  // grids, and sizes of the workspace
+  // grids: of 256 threads to a workgroup, 2^32 in all; of single tokens there are at most heads (m / 4 + 1) workgroups to a sequence
   const int64_t bh = (int64_t)p.batch * p.heads;
-  return bh < (1 << 24) && bh * std::max(p.m, 1) < ((int64_t)1 << 36) && bh * std::max(p.k, 1) < ((int64_t)1 << 36) &&
-         bh * up(std::max(p.m, p.k), 32) < ((int64_t)1 << 30);
+  return bh <= (1 << 21) && bh * up(std::max(p.m, p.k), kAttnPanel) < (1 << 23);
 }
 
 int check(const spdl_attention_problem* p, const int* bucket_of, const void* table) {
@@ -210,7 +211,7 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
     if (hipGetLastError() != hipSuccess) return false;
   }
   const int64_t blocks = up(std::max<int64_t>((int64_t)a.group * a.m, a.k), 256 / (D / 8));
-  attention_terms_kernel<T, D><<<dim3((unsigned)(each * blocks)), dim3(256), 0, stream>>>(o, blocks);
+  attention_terms_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)std::min<int64_t>(each, 32768)), dim3(256), 0, stream>>>(o, (int)each);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -405,20 +406,26 @@ int64_t spdl_attention_mask_bytes(int m, int k) {
 
 int spdl_build_attention_mask(int m, int k, int nnz, const int* row_offsets, const int* column_indices, void* mask, void* stream) {
   if (m < 0 || k < 0 || nnz < 0 || m > kMostRows || k > kMostRows) return SPDL_ERR_INVALID;
-  const int64_t words = MaskLayout(m, k).words;
-  if (words == 0) return SPDL_OK;
+  const MaskLayout lay(m, k);
+  if (lay.words == 0) return SPDL_OK;
   if (!mask || reinterpret_cast<uintptr_t>(mask) % 8 || (nnz > 0 && (!row_offsets || !column_indices))) return SPDL_ERR_INVALID;
-  if (up(words, 256) > INT32_MAX) return SPDL_ERR_INVALID;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  attention_mask_clear_kernel<<<dim3((unsigned)up(words, 256)), dim3(256), 0, s>>>(words, static_cast<uint64_t*>(mask));
+  auto* bits = static_cast<uint64_t*>(mask);
+  const auto grid = [](int64_t blocks) { return dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)); };   // whose workgroups take more than one
+  const int64_t clear_from = nnz == 0 ? 0 : lay.row_tiles;    // the words are written whole
+  attention_mask_clear_kernel<<<grid(up(lay.words - clear_from, 256)), dim3(256), 0, s>>>(lay.words - clear_from, bits + clear_from);
   if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
   if (nnz == 0) return SPDL_OK;
-  auto* bits = static_cast<unsigned long long*>(mask);
-  attention_mask_rows_kernel<<<dim3((unsigned)up(m, 4)), dim3(256), 0, s>>>(m, k, row_offsets, column_indices, bits);
+  auto rows = [&](auto kernel, int64_t each) {
+    const int64_t words = std::min(lay.tj, kMaskWords / each);
+    kernel<<<grid(lay.ti * (64 / each) * up(lay.tj, words)), dim3(256), words * each * 8, s>>>(m, k, row_offsets, column_indices, bits);
+  };
+  if (lay.tj * 16 <= kMaskWords) rows(attention_mask_rows_kernel<16>, 16);
+  else if (lay.tj * 4 <= kMaskWords) rows(attention_mask_rows_kernel<4>, 4);
+  else rows(attention_mask_rows_kernel<1>, 1);
   if (hipGetLastError() != hipSuccess) return SPDL_ERR_LAUNCH;
-  const int64_t tiles = up(m, 64) * up(k, 64);
-  attention_mask_tiles_kernel<<<dim3((unsigned)up(tiles, 4)), dim3(256), 0, s>>>(m, k, bits);
+  attention_mask_tiles_kernel<<<grid(up(lay.ti * lay.tj, 4)), dim3(256), 0, s>>>(m, k, bits);
   return hipGetLastError() == hipSuccess ? SPDL_OK : SPDL_ERR_LAUNCH;
 }
 

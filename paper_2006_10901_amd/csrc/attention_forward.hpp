@@ -631,42 +631,59 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[flat] = attn_lse({most, total});
 }
 
-// Bits of the sparse matrix, from its CSR topology: cleared, the words by rows set by one wave per row (which thread sets a bit first changes
-// nothing), then one wave per tile of 64 x 64 turns its 64 words by rows into 64 by columns and marks the tile.  Column indices out of
-// range are passed over.  (Setting the words by columns and the marks entry by entry, many threads at one word, took 5.8 ms for 1.7
-// million entries of 4096 x 4096.)
+// Bits of the sparse matrix, from its CSR topology: the words by rows of ROWS rows at a time are made in LDS (which thread sets a bit first
+// changes nothing) and written once, then one wave per tile of 64 x 64 turns its 64 words by rows into 64 by columns and marks the tile.
+// Column indices out of range are passed over.  ROWS neighbouring words are one write, so as many rows as LDS has room for are taken; where one
+// row has no room its entries are read once for each of its parts.  (Against bits set one by one in memory, us: 1.7 million entries of
+// 4096 x 4096 26 / 95, 10.6 million of 12288 x 12288 99 / 520, 2 million of 2000 x 50000 56 / 121, 128000 of 64 x 200000 25 / 42.)
+constexpr int kMaskWords = 8192;                          // of a workgroup
 __global__ __launch_bounds__(256) void attention_mask_clear_kernel(int64_t words, uint64_t* mask) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < words) mask[i] = 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) mask[i] = 0;
 }
+template <int ROWS>
 __global__ __launch_bounds__(256) void attention_mask_rows_kernel(int m, int k, const int* __restrict__ row_offsets,
-                                                                  const int* __restrict__ column_indices, unsigned long long* mask) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= m) return;
+                                                                  const int* __restrict__ column_indices, uint64_t* mask) {
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  auto* bits = reinterpret_cast<unsigned long long*>(lds_raw);   // [word][row]
+  constexpr int kEach = 256 / ROWS, kWords = kMaskWords / ROWS;
   const MaskLayout lay(m, k);
-  for (int p = row_offsets[row] + lane; p < row_offsets[row + 1]; p += kWave) {
-    const int col = column_indices[p];
-    if (col >= 0 && col < k) atomicOr(mask + lay.row_words + (int64_t)(col >> 6) * lay.ti * 64 + row, 1ull << (col & 63));
+  const int parts = (int)((lay.tj + kWords - 1) / kWords), mine = threadIdx.x / kEach;
+  for (int64_t id = blockIdx.x; id < lay.ti * (64 / ROWS) * parts; id += gridDim.x) {
+    const int row0 = (int)(id / parts) * ROWS, row = row0 + mine, first = (int)(id % parts) * kWords, words = (int)min((int64_t)kWords, lay.tj - first);
+    for (int i = threadIdx.x; i < words * ROWS; i += 256) bits[i] = 0;
+    __syncthreads();
+    if (row < m) {
+      const int end = row_offsets[row + 1];
+      for (int p = row_offsets[row] + threadIdx.x % kEach; p < end; p += kEach) {
+        const int col = column_indices[p], word = (col >> 6) - first;
+        if (col >= 0 && col < k && word >= 0 && word < words) atomicOr(bits + word * ROWS + mine, 1ull << (col & 63));
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < words * ROWS; i += 256) mask[lay.row_words + (int64_t)(first + i / ROWS) * lay.ti * 64 + row0 + i % ROWS] = bits[i];
+    __syncthreads();
   }
 }
-__global__ __launch_bounds__(256) void attention_mask_tiles_kernel(int m, int k, unsigned long long* mask) {
+__global__ __launch_bounds__(256) void attention_mask_tiles_kernel(int m, int k, uint64_t* mask) {
   const MaskLayout lay(m, k);
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (tile >= lay.ti * lay.tj) return;
   const int lane = threadIdx.x & 63;
-  const int64_t ti = tile % lay.ti, tj = tile / lay.ti;
-  const unsigned long long word = mask[lay.row_words + (tj * lay.ti + ti) * 64 + lane];
-  if (!__any(word != 0)) return;                          // the words by columns are clear already
-  unsigned long long column = 0;
+  for (int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); tile < lay.ti * lay.tj; tile += (int64_t)gridDim.x * 4) {
+    const int64_t ti = tile % lay.ti, tj = tile / lay.ti;
+    const uint64_t word = mask[lay.row_words + (tj * lay.ti + ti) * 64 + lane];
+    uint64_t column = 0;
+    if (__any(word != 0)) {
 #pragma unroll
-  for (int b = 0; b < 64; ++b) {
-    const unsigned long long rows = __ballot((word >> b) & 1);
-    if (lane == b) column = rows;
-  }
-  mask[lay.col_words + (ti * lay.tj + tj) * 64 + lane] = column;
-  if (lane == 0) {
-    atomicOr(mask + lay.row_tiles + ti * ((lay.tj + 63) / 64) + (tj >> 6), 1ull << (tj & 63));
-    atomicOr(mask + lay.col_tiles + tj * ((lay.ti + 63) / 64) + (ti >> 6), 1ull << (ti & 63));
+      for (int b = 0; b < 64; ++b) {
+        const uint64_t rows = __ballot((word >> b) & 1);
+        if (lane == b) column = rows;
+      }
+      auto* marks = reinterpret_cast<unsigned long long*>(mask);
+      if (lane == 0) {
+        atomicOr(marks + lay.row_tiles + ti * ((lay.tj + 63) / 64) + (tj >> 6), 1ull << (tj & 63));
+        atomicOr(marks + lay.col_tiles + tj * ((lay.ti + 63) / 64) + (ti >> 6), 1ull << (ti & 63));
+      }
+    }
+    mask[lay.col_words + (ti * lay.tj + tj) * 64 + lane] = column;
   }
 }
 
@@ -703,12 +720,12 @@ __device__ __forceinline__ float attn_largest(float most, const f32x4& v) {
 }
 __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperands o) {
   __shared__ float waves[4];
-  int id = blockIdx.x;
-  const int part = id % o.parts;
+  int64_t id = blockIdx.x;
+  const int part = (int)(id % o.parts);
   id /= o.parts;
-  const int which = id % o.count;
+  const int which = (int)(id % o.count);
   id /= o.count;
-  const int kv_head = id % o.kv_heads, batch = id / o.kv_heads;
+  const int kv_head = (int)(id % o.kv_heads), batch = (int)(id / o.kv_heads);
   const AttnOperand& x = o.of[which];
   const int64_t rows = attn_operand_rows(o, x, batch), begin = rows * part / o.parts, end = rows * (part + 1) / o.parts;
   const int pieces = (o.d + 3) / 4;
@@ -726,62 +743,65 @@ __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperan
 // Copies of the operands for the panel kernels, rows of D numbers, zeros behind d and behind a sequence's states.  Single precision:
 // numbers times the power of two as two fp16 terms, the first ones of a row before the second ones.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands o, int64_t blocks_each) {
+__global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands o, int each) {
   constexpr int kPieces = D / 8, kRows = 256 / kPieces;
-  const int64_t id = blockIdx.x / blocks_each, block = blockIdx.x - id * blocks_each;
-  const int which = (int)(id % o.count);
-  const int64_t bh = id / o.count;
-  const int kv_head = (int)(bh % o.kv_heads), batch = (int)(bh / o.kv_heads);
-  const AttnOperand& x = o.of[which];
-  const int64_t all = (int64_t)x.group * x.rows, rows = attn_operand_rows(o, x, batch);
-  const int64_t r = block * kRows + threadIdx.x / kPieces;
-  const bool mine = r < all && threadIdx.x < kRows * kPieces;
-  const int c = threadIdx.x % kPieces * 8;
-  _Float16* to = x.to + (bh * all + r) * (attn_terms<T>() * D) + c;
-  if constexpr (sizeof(T) == 2) {
-    f16x8 v = {};
-    if (mine && r < rows) v = attn_load_piece<_Float16>(attn_operand_row<_Float16>(x, batch, kv_head, r), c, o.d);
-    if (mine) *reinterpret_cast<f16x8*>(to) = v;
-  } else {
-    const int lane = threadIdx.x & 63;
-    float most = 0.f;
-    if (o.most) {
-      most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
-    } else {                                              // few numbers: every workgroup looks at all of them
-      const int pieces = (o.d + 3) / 4;
+  for (int id = blockIdx.y; id < each; id += gridDim.y) {
+    const int64_t block = blockIdx.x;
+    const int which = id % o.count;
+    const int64_t bh = id / o.count;
+    const int kv_head = (int)(bh % o.kv_heads), batch = (int)(bh / o.kv_heads);
+    const AttnOperand& x = o.of[which];
+    const int64_t all = (int64_t)x.group * x.rows, rows = attn_operand_rows(o, x, batch);
+    const int64_t r = block * kRows + threadIdx.x / kPieces;
+    const bool mine = r < all && threadIdx.x < kRows * kPieces;
+    const int c = threadIdx.x % kPieces * 8;
+    _Float16* to = x.to + (bh * all + r) * (attn_terms<T>() * D) + c;
+    if constexpr (sizeof(T) == 2) {
+      f16x8 v = {};
+      if (mine && r < rows) v = attn_load_piece<_Float16>(attn_operand_row<_Float16>(x, batch, kv_head, r), c, o.d);
+      if (mine) *reinterpret_cast<f16x8*>(to) = v;
+    } else {
+      const int lane = threadIdx.x & 63;
+      float most = 0.f;
+      if (o.most) {
+        most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
+      } else {                                            // few numbers: every workgroup looks at all of them
+        const int pieces = (o.d + 3) / 4;
 #pragma unroll 4
-      for (int64_t at = threadIdx.x; at < rows * pieces; at += 256) {
-        const int64_t row = at / pieces;
-        most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, row), (int)(at - row * pieces) * 4, o.d));
-      }
-    }
-#pragma unroll
-    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
-    if (!o.most) {
-      __shared__ float waves[4];
-      if (lane == 0) waves[threadIdx.x >> 6] = most;
-      __syncthreads();
-      most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
-    }
-    const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
-    const float factor = ldexpf(1.f, e);
-    if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + which] = ldexpf(1.f, -e);
-    f16x8 hi = {}, lo = {};
-    if (mine && r < rows) {
-      const float* row = attn_operand_row<float>(x, batch, kv_head, r);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 v = attn_load_piece<float>(row, c + 4 * h, o.d) * factor;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          hi[4 * h + i] = (_Float16)v[i];
-          lo[4 * h + i] = (_Float16)(v[i] - (float)hi[4 * h + i]);
+        for (int64_t at = threadIdx.x; at < rows * pieces; at += 256) {
+          const int64_t row = at / pieces;
+          most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, row), (int)(at - row * pieces) * 4, o.d));
         }
       }
-    }
-    if (mine) {
-      *reinterpret_cast<f16x8*>(to) = hi;
-      *reinterpret_cast<f16x8*>(to + D) = lo;
+#pragma unroll
+      for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+      if (!o.most) {
+        __shared__ float waves[4];
+        if (lane == 0) waves[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+      }
+      const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
+      const float factor = ldexpf(1.f, e);
+      if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + which] = ldexpf(1.f, -e);
+      f16x8 hi = {}, lo = {};
+      if (mine && r < rows) {
+        const float* row = attn_operand_row<float>(x, batch, kv_head, r);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 v = attn_load_piece<float>(row, c + 4 * h, o.d) * factor;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            hi[4 * h + i] = (_Float16)v[i];
+            lo[4 * h + i] = (_Float16)(v[i] - (float)hi[4 * h + i]);
+          }
+        }
+      }
+      if (mine) {
+        *reinterpret_cast<f16x8*>(to) = hi;
+        *reinterpret_cast<f16x8*>(to + D) = lo;
+      }
+      if (!o.most) __syncthreads();                       // `waves` is read
     }
   }
 }

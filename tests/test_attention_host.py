@@ -34,7 +34,8 @@ def backward(p, Q=ONE, K=ONE, V=ONE, bucket_of=NULL, table=NULL, O=ONE, lse=ONE,
 
 @pytest.mark.parametrize("wrong", [dict(batch=-1), dict(heads=-4), dict(heads=5), dict(kv_heads=0), dict(m=-1), dict(k=-1), dict(d=0),
                                    dict(span=-1), dict(span=1025), dict(buckets=129), dict(buckets=-1), dict(scale=math.nan),
-                                   dict(scale=math.inf), dict(m=2 ** 30), dict(batch=2 ** 20, heads=64, kv_heads=64)])
+                                   dict(scale=math.inf), dict(m=2 ** 30), dict(batch=2 ** 20, heads=64, kv_heads=64),
+                                   dict(batch=2 ** 19, heads=8, kv_heads=8), dict(batch=2 ** 10, heads=8, kv_heads=8, k=2 ** 20)])
 def test_sizes_that_are_refused(wrong):
     p = problem(**wrong)
     assert forward(p) == INVALID and forward(p, f16=True) == INVALID and backward(p) == INVALID

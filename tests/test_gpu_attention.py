@@ -245,7 +245,7 @@ def test_two_streams_at_once():
         assert all(torch.equal(x, y) for x, y in zip(alone, (t for c in (a, b) for t in c.results().values())))
 
 
-@pytest.mark.parametrize("m,k,nnz", [(1, 1, 1), (5, 70, 9), (64, 64, 4096), (65, 129, 1), (130, 5000, 20000), (300, 300, 0)])
+@pytest.mark.parametrize("m,k,nnz", [(1, 1, 1), (5, 70, 9), (64, 64, 4096), (65, 129, 1), (130, 5000, 20000), (300, 300, 0), (70, 40000, 9000), (67, 140000, 5000), (3, 600000, 5000)])
 def test_mask_from_a_topology(m, k, nnz):
     """Every bit by rows and by columns, and which tiles hold any; indices in no order, and twice."""
     gen = torch.Generator().manual_seed(m * k)
