@@ -400,6 +400,18 @@ struct AttnSeenTiles {
     a = b = mask + at + (first_row >> 6) * per;
     if ((first_row >> 6) + 1 < sets) b = a + per;
   }
+  // the one tile below `end` that the first (or second) 64 rows see, or -1 if they see none or more
+  __device__ __forceinline__ int only(bool second, int end) const {
+    if (!a) return end == 1 ? 0 : -1;
+    int found = -1;
+    for (int g = 0; g * 64 < end; ++g) {
+      const uint64_t x = (second ? b : a)[g];
+      if (!x) continue;
+      if (found >= 0 || (x & (x - 1))) return -1;
+      found = uniform(g * 64 + (int)__builtin_ctzll(x));
+    }
+    return found < end ? found : -1;
+  }
   // the next one from t on, or `end`
   __device__ __forceinline__ int next(int t, int end) {
     if (!a) return t;

@@ -167,6 +167,19 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     position = attn_position(a, batch);
   }
   AttnRowSums sums = {};
+  // Half precision: the rounding of O costs D as much as sqrt(keys) times what rounding dS costs, so that rows of few keys take D as
+  // (sum P dP) / (sum P), from products formed twice, where all keys lie in one tile (2-norm of dQ, in units of what rounding it costs: 2 / 5 / 20
+  // keys 2.5 / 1.7 / 1.48 with D = dO . O, 1.42 so; 65 1.46)
+  const int only = kTerms == 1 ? tiles.only(wave >= 2, (seen + kAttnTile - 1) / kAttnTile) : -1;
+  const bool tells = only < 0 ? at.split == 0 : begin <= only && only < end;   // the part of the keys that knows D
+  // products become weights; whether the block lies at an end of the bias
+  auto weigh = [&](f32x16& x, int near) {
+    const bool far = BIAS && attn_far(near, a.span);
+    if (!BIAS) own.weights(x, 0.f);
+    else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
+    else own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+    return far;
+  };
   float to_ds = own.to_dp, delta_ds = delta, from_ds = 1.f;   // what makes dS, taken times the factor of ds_scale
 
   f32x16 acc[D / 32] = {};
@@ -195,6 +208,26 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     if (t < end) load(t);
     if (wave_row >= a.m || !__any(word != 0)) continue;
     const bool hide = __any(word != ~0ull);
+    if (kTerms == 1 && key0 == only * kAttnTile) {
+      float sum_p = 0.f, sum = 0.f;
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        f32x16 x = {}, y = {};
+        attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+        attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+        weigh(x, key0 + 32 * b - (position + wave_row));
+        const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sum_p += attn_select(w, r, x[r], 0.f);
+          sum += attn_select(w, r, x[r] * y[r], 0.f);
+        }
+      }
+      sum_p = attn_sum_halves(sum_p);
+      sum = attn_sum_halves(sum) * own.to_dp;
+      if (sum_p > 0.f) delta = sum / sum_p;
+      delta_ds = delta * ds_scale.factor;
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int near = key0 + 32 * b - (position + wave_row);   // relative position of the block's first key and first query
@@ -202,10 +235,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
       attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
       attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
       __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
-      const bool far = BIAS && attn_far(near, a.span);
-      if (!BIAS) own.weights(x, 0.f);
-      else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
-      else own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+      const bool far = weigh(x, near);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
       const bool sum_weights = kTerms == 2 || far;
       if (hide && sum_weights) {
@@ -255,13 +285,13 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
       weight = (float)attn_row_weight<T>(all);
       if (valid && half == 0) attn_finish_row<T, BIAS>(a, own.flat, delta, all);
     } else if (valid && half == 0) {
-      if (at.split == 0) a.delta[own.flat] = delta;
+      if (tells) a.delta[own.flat] = delta;
       double* to = a.row_sums + (at.split * rows + own.flat) * kAttnRowSums;
 #pragma unroll
       for (int i = 0; i < kAttnRowSums; ++i)
         if (BIAS || i < 2) to[i] = s[i];
     }
-  } else if (valid && half == 0 && at.split == 0) {
+  } else if (valid && half == 0 && tells) {
     a.delta[own.flat] = delta;
   }
   if (a.mask) {
