@@ -260,23 +260,29 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  * with g = h / (heads / kv_heads): consecutive query heads share a head of K and V.  A row that sees nothing, or whose scores are all
  * -inf, has O = 0, lse = -inf and no part in any gradient.
  *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads), 1 <= d <= 128
- *     (SPDL_ERR_UNSUPPORTED above).  scale: finite.  span (0 .. 1024) and buckets (1 .. 128) are those of the bias.
+ *     (SPDL_ERR_UNSUPPORTED above); batch*heads <= 2^21, batch*heads*ceil(max(m, k) / 128) < 2^23.  scale: finite.
+ *     span (0 .. 1024) and buckets (1 .. 128) are those of the bias.
  *     Strides, in elements, of [batch, head, row] for each tensor; the d elements of a row lie next to one another.  Those of inputs
  *     are >= 0 (0: the same for all); the elements of an output must not share addresses.  Only the strides of tensors that a
  *     call takes are looked at.
  *   Q, O, dO, dQ : DEVICE, [batch, heads, m, d].  K, V, dK, dV : DEVICE, [batch, kv_heads, k, d].  lse : DEVICE fp32[batch*heads*m];
  *     may be NULL in the forward pass.  Base pointers are aligned to their element type; pieces of 16 bytes may start anywhere.
+ *     Outputs and the workspace overlap neither one another nor an input.
  *   lengths : DEVICE int32[batch], how many states each sequence has (taken as 0 below 0, as k above k); NULL: k of each.  What lies
  *     in K and V behind a sequence's states is not read.
  *   mask : DEVICE, from spdl_build_attention_mask for this m and k; NULL: every position.  One for all sequences and heads.
  *   bucket_of : DEVICE int32[2*span+1], each in [0, buckets) (spdl_build_relative_buckets_host);  table : DEVICE [heads*buckets].
- *     Both NULL: no bias.  A bias of -inf hides a position.
+ *     Both NULL: no bias.  A bias of -inf gives a position the weight 0.
  *   positions : DEVICE int32[batch], the position of query 0 among the states (a decoding step's m newest of L: L - m); NULL: 0.
  *   workspace : DEVICE, spdl_attention_workspace bytes, 16-byte aligned; NULL where that is 0.  Its content before a call does not
  *     matter; calls that may run at the same time need one each.
- * Products and sums: fp32 in the fp32 functions.  In the _f16 ones products of binary16 and fp32 sums; weights P, and dS in the
- * gradients, are rounded to binary16 (taken times a power of two that keeps them in its range) before they are multiplied; results are
- * rounded once.  Results do not depend on how the work is split between workgroups beyond the order of sums, and are deterministic.
+ * Precision: all sums are fp32 or wider.  In the fp32 functions every factor of a product counts to 2^-23 of itself, or to 2^-39 of the
+ * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V; of K and V: in a head; of P and dS: in
+ * a row or a block of rows).  In the _f16 ones weights P, and dS in the gradients, are rounded to binary16 (taken times a power of two
+ * that keeps them in its range) before they are multiplied, and results are rounded once.  Two calls on the same inputs give the same bits.
+ * Inf and NaN: a row that does not see a state, by its mask or the sequence's length, is not touched by what stands there, and neither
+ * are gradients; with a mask, rows that such numbers would reach otherwise are formed again one position at a time, at the speed of
+ * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.
  * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once.  */
 typedef struct { int64_t batch, head, row; } spdl_strides;
 typedef struct {

@@ -9,7 +9,6 @@
 #include "attention_backward.hpp"
 #include "attention_forward.hpp"
 
-
 namespace {
 
 using namespace spdl;

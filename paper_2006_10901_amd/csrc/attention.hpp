@@ -139,7 +139,8 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
     if (rows >= ROWS && d * (int)sizeof(T) == BYTES) {
 #pragma unroll
       for (int i = 0; i < kCount; ++i)
-        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(from + (kEven ? i * (THREADS / kPieces) * stride * (int)sizeof(T) : 0) + whole.v[kEven ? 0 : i]);
+        v[i] = *reinterpret_cast<const typename AttnPiece<T>::Any*>(from + (kEven ? i * (THREADS / kPieces) * stride * (int)sizeof(T) : 0) +
+                                                                    whole.v[kEven ? 0 : i]);
     } else {
       asm volatile("");
 #pragma unroll
@@ -624,7 +625,8 @@ __device__ __forceinline__ void attn_exact_dq(const AttnArgs& a, int batch, int 
 
 // dK and dV of one key over the tiles [begin, end) of all heads of the group (see attention_dkv_kernel).
 template <typename T, typename OUT>
-__device__ __forceinline__ void attn_exact_dkv(const AttnArgs& a, int batch, int kv_head, int key, int64_t begin, int64_t end, OUT* dk_to, OUT* dv_to, int lane) {
+__device__ __forceinline__ void attn_exact_dkv(const AttnArgs& a, int batch, int kv_head, int key, int64_t begin, int64_t end, OUT* dk_to, OUT* dv_to,
+                                               int lane) {
   const MaskLayout lay(a.m, a.k);
   const int tiles = (a.m + 63) / 64;
   const AttnLane k = attn_lane_row(attn_row<T>(a.K, a.kk, batch, kv_head, key), a.d, lane);

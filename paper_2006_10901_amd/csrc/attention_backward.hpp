@@ -1,8 +1,8 @@
 // Gradients of attention.  With P = exp(s - lse), D_i = dO_i . O_i and dS_ij = P_ij (dO_i . V_j - D_i):
 //   dV_j = sum_i P_ij dO_i,   dK_j = scale sum_i dS_ij Q_i,   dQ_i = scale sum_j dS_ij K_j,   dtable[bucket] = sum of dS over its positions.
 // Two kernels form the scores again, one by panels of queries (dQ, and D, which it leaves for the others), one by panels of keys (dK
-// and dV): each sum has one owner, so that nothing is added up in an order that changes from call to call.  A third goes over the
-// positions near the diagonal for the gradient of the bias.
+// and dV): each sum has one owner, so that nothing is added up in an order that changes from call to call.  More workgroups of the
+// second's launch go over the positions near the diagonal for the gradient of the bias, a sum per relative position.
 #pragma once
 #include "attention.hpp"
 
@@ -643,11 +643,13 @@ __global__ __launch_bounds__(256) void attention_dkv_again_kernel(const AttnArgs
   for (; left; left &= left - 1) {
     const int key = panel * kAttnPanel + wave * 32 + __builtin_ctz(left);
     if (a.splits == 1) {
-      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, static_cast<T*>(a.dK) + place.batch * a.dk.batch + place.kv_head * a.dk.head + (int64_t)key * a.dk.row,
-                        static_cast<T*>(a.dV) + place.batch * a.dv.batch + place.kv_head * a.dv.head + (int64_t)key * a.dv.row, lane);
+      T* dK = static_cast<T*>(a.dK) + place.batch * a.dk.batch + place.kv_head * a.dk.head + (int64_t)key * a.dk.row;
+      T* dV = static_cast<T*>(a.dV) + place.batch * a.dv.batch + place.kv_head * a.dv.head + (int64_t)key * a.dv.row;
+      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, dK, dV, lane);
     } else {
       const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k, flat = ((int64_t)place.batch * a.kv_heads + place.kv_head) * a.k + key;
-      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, a.part + (split * rows + flat) * a.d, a.part + ((a.splits + split) * rows + flat) * a.d, lane);
+      float *dK = a.part + (split * rows + flat) * a.d, *dV = a.part + ((a.splits + split) * rows + flat) * a.d;
+      attn_exact_dkv<T>(a, place.batch, place.kv_head, key, begin, end, dK, dV, lane);
     }
   }
 }

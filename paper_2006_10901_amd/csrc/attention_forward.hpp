@@ -223,8 +223,8 @@ template <int N> __device__ __forceinline__ float token_rotate(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
 }
 
-// More than 4 rows of a head of K and V, in half precision: 32 to a workgroup.  K and V are read once per 32 rows.  The four waves take blocks of 32 keys in turn, each with its own statistics, and no wave waits for another
-// before the end.
+// More than 4 rows of a head of K and V, in half precision: 32 to a workgroup.  K and V are read once per 32 rows.  The four waves take
+// blocks of 32 keys in turn, each with its own statistics, and no wave waits for another before the end.
 template <int D, bool BIAS>
 __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attention_tokens_kernel(const AttnArgs a) {
   using T = _Float16;
@@ -633,8 +633,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
 
 // Bits of the sparse matrix, from its CSR topology: the words by rows of ROWS rows at a time are made in LDS (which thread sets a bit first
 // changes nothing) and written once, then one wave per tile of 64 x 64 turns its 64 words by rows into 64 by columns and marks the tile.
-// Column indices out of range are passed over.  ROWS neighbouring words are one write, so as many rows as LDS has room for are taken; where one
-// row has no room its entries are read once for each of its parts.  (Against bits set one by one in memory, us: 1.7 million entries of
+// Column indices out of range are passed over.  ROWS neighbouring words are one write, so as many rows as LDS has room for are taken;
+// where one row has no room its entries are read once for each of its parts.  (Against bits set one by one in memory, us: 1.7 million entries of
 // 4096 x 4096 26 / 95, 10.6 million of 12288 x 12288 99 / 520, 2 million of 2000 x 50000 56 / 121, 128000 of 64 x 200000 25 / 42.)
 constexpr int kMaskWords = 8192;                          // of a workgroup
 __global__ __launch_bounds__(256) void attention_mask_clear_kernel(int64_t words, uint64_t* mask) {
@@ -660,7 +660,8 @@ __global__ __launch_bounds__(256) void attention_mask_rows_kernel(int m, int k, 
       }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < words * ROWS; i += 256) mask[lay.row_words + (int64_t)(first + i / ROWS) * lay.ti * 64 + row0 + i % ROWS] = bits[i];
+    for (int i = threadIdx.x; i < words * ROWS; i += 256)
+      mask[lay.row_words + (int64_t)(first + i / ROWS) * lay.ti * 64 + row0 + i % ROWS] = bits[i];
     __syncthreads();
   }
 }

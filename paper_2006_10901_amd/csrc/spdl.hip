@@ -1771,7 +1771,7 @@ const char* spdl_status_string(int status) {
   }
 }
 
-int spdl_version(void) { return 140; }
+int spdl_version(void) { return 150; }
 
 }  // extern "C"
 

@@ -35,6 +35,26 @@ def test_lengths(dtype, m, k, bias):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,heads,m", [(65, 2, 1), (65, 1, 40), (64, 8, 1), (9, 16, 130)])
+def test_many_sequences_of_unequal_length(dtype, batch, heads, m):
+    lengths = [(37 * b) % 150 for b in range(batch)]
+    Case(dtype, batch=batch, heads=heads, m=m, k=149, d=32, lengths=lengths, buckets=8, span=20, seed=batch).check(what=f"{dtype} {batch} x {heads} x {m}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,m,k", [(2, 0, 70), (2, 9, 0), (2, 40, 0), (0, 9, 70)])
+@pytest.mark.parametrize("mask", [None, causal], ids=["all", "causal"])
+def test_nothing_to_attend(dtype, batch, m, k, mask):
+    """No queries: the states' gradients are 0.  No states: results of 0, as for any row that sees nothing.  The table's gradient is 0."""
+    case = Case(dtype, batch=batch, heads=2, m=m, k=k, d=32, mask=mask, buckets=8, span=20).prepare()
+    case.forward()
+    case.backward()
+    for name, got in case.results().items():
+        want = torch.full_like(got, float("-inf")) if name == "lse" else torch.zeros_like(got)
+        assert torch.equal(got, want), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("mask", [banded, causal, blocks, nothing, sparse_rows], ids=lambda f: f.__name__)
 @pytest.mark.parametrize("m,k", [(1, 200), (9, 129), (130, 260), (333, 333), (64, 5000)])
 def test_masks(dtype, mask, m, k):
