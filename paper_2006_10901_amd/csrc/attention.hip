@@ -43,11 +43,14 @@ inline int64_t take(int64_t& end, int64_t floats) {
   return at;
 }
 
-// How many workgroups a panel's work is split over: enough to give every compute unit `want` of them, of at least `least` steps each, if
-// there are `from` steps, so that what is saved pays for the kernel that joins the parts.
-inline int split_count(int64_t blocks, int64_t steps, int want, int least, int from) {
+// How many workgroups a panel's work is split over: enough to give every compute unit the `each` that it holds at a time, of at least
+// `least` steps, and two of at least six if it holds one; if there are `from` steps, so that what is saved pays for the kernel that joins the
+// parts.  (One at a time, us, 1 / 2 for each compute unit: fp32, 8 heads of 128 on one of 685 x 942, 15 tiles 41 / 54; 8 of 96 of 1277 x 294,
+// training, 142 / 165; but 5 masked heads of 96 of 2627 x 2627, 41 tiles, 84 / 76, and fp16, 8 x 8 heads of 128 of 1188 x 1104 414 / 372.)
+inline int split_count(int64_t blocks, int64_t steps, int each, int least, int from) {
   if (blocks <= 0 || steps < from) return 1;
-  const int64_t s = std::min<int64_t>(want * 256 / blocks, steps / least);
+  int64_t s = std::min<int64_t>(each * 256 / blocks, steps / least);
+  if (each == 1) s = std::max(s, std::min<int64_t>(2 * 256 / blocks, steps / 6));
   return (int)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
 
@@ -63,18 +66,19 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   // 2 heads of 22 x 1505 65 / 62 / 67; single tokens, 4 / 8 blocks of 32 keys: fp32 2 x 4 heads on 361 keys 18 / 26, fp16 7 x 14 rows on 3547 23 / 19).
   const bool f32 = elem_bytes == 4;
   const int least = f32 ? 1 : 2, from = f32 ? 3 : 6;
+  const int each = x.width * (f32 ? 2 : 1) <= 128 ? 2 : 1;    // the launch bounds of the panel kernels
   if (x.token) {
     x.token_rows = group * p.m <= 4 ? 4 : !f32 ? 32 : group * p.m <= 8 ? 8 : 16;
     x.forward_blocks = (int64_t)p.batch * p.kv_heads * up(group * p.m, x.token_rows);
     x.forward_splits = split_count(x.forward_blocks, up(p.k, 32), 2, f32 ? 4 : 8, f32 ? 9 : 17);
   } else {
     x.forward_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), 2, least, from);
+    x.forward_splits = split_count(x.forward_blocks, up(p.k, kAttnTile), each, least, from);
   }
   x.dq_blocks = (int64_t)p.batch * p.heads * up(p.m, kAttnPanel);
-  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), 2, least, from);
+  x.dq_splits = split_count(x.dq_blocks, up(p.k, kAttnTile), each, least, from);
   x.dkv_blocks = (int64_t)p.batch * p.kv_heads * up(p.k, kAttnPanel);
-  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), 2, least, from);
+  x.dkv_splits = split_count(x.dkv_blocks, group * up(p.m, kAttnTile), x.width == 128 ? 1 : each, least, from);
   // tiles near the diagonal that a panel meets
   x.dbias_splits = split_count(x.dq_blocks, std::min<int64_t>(up(p.k, kAttnTile), (2 * p.span + kAttnPanel) / kAttnTile + 2), 2, 1, 3);
   x.parts = (int64_t)p.batch * up(p.m, kAttnPanel) * x.dbias_splits;
