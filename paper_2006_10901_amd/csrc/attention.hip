@@ -239,7 +239,7 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
     return launch(attention_token_kernel<T, D, 4, BIAS>, blocks, lds, a, stream);
   }
   if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
-  using Tile = AttnTile<D, attn_terms<T>()>;
+  using Tile = AttnTile<D, attn_terms<T>(), attn_queries_each<T, D>()>;
   const int lds = Tile::kSets * kAttnTile * (Tile::kPitch + Tile::kPitchT) + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
   a.again = reinterpret_cast<unsigned*>(w + x.forward_again);
   if (!launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream)) return false;
@@ -248,8 +248,8 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
 
 template <typename T, int D, bool BIAS>
 bool launch_backward(const Plan& x, AttnArgs a, char* w, void* dtable, hipStream_t stream) {
-  using Tile = AttnTile<D, attn_terms<T>()>;
-  constexpr int kTiles = Tile::kSets * Tile::kPair;
+  using Queries = AttnTile<D, attn_terms<T>(), attn_queries_each<T, D>()>;
+  using Keys = AttnTile<D, attn_terms<T>(), attn_keys_each<T, D>()>;
   const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
   const int64_t pieces = up(a.d, 4);
   a.part = reinterpret_cast<float*>(w + x.part);
@@ -257,7 +257,7 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, void* dtable, hipStream
   if ((x.dq_blocks > 0 || x.dkv_blocks > 0) && !prepare_operands<T, D>(x, a, w, true, stream)) return false;
   if (x.dq_blocks > 0) {
     a.splits = x.dq_splits;
-    if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, kTiles + bias, a, stream)) return false;
+    if (!launch(attention_dq_kernel<T, D, BIAS>, x.dq_blocks * a.splits, Queries::kSets * Queries::kPair + bias, a, stream)) return false;
     if (a.mask && !launch(attention_dq_again_kernel<T>, x.dq_blocks * a.splits, 0, a, stream)) return false;
     if (a.splits > 1) {
       attention_sum_dq_kernel<T, BIAS, attn_row_sums<T, BIAS>()><<<dim3((unsigned)up(x.rows * pieces, 256)), dim3(256), 0, stream>>>(a);
@@ -267,8 +267,9 @@ bool launch_backward(const Plan& x, AttnArgs a, char* w, void* dtable, hipStream
   // dK and dV, and in the same launch the sums for the bias, unless the LDS that those take would leave fewer workgroups to a compute unit
   a.splits = x.dkv_splits, a.bias_splits = x.dbias_splits;
   const int64_t blocks = x.dkv_blocks * a.splits, bias_blocks = BIAS && a.part_bias ? x.dq_blocks * a.bias_splits : 0;
-  const int lds = kTiles + Tile::kSets * 5 * kAttnTile * 4 + bias, bias_lds = Tile::kPair + bias + 16 + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
-  const bool together = bias_blocks > 0 && std::max(lds, bias_lds) * attn_dkv_each<T, D>() <= 160 * 1024;
+  const int lds = Keys::kSets * (Keys::kPair + 5 * kAttnTile * 4) + bias;
+  const int bias_lds = Keys::kPair + bias + 16 + kAttnWaves * (kAttnDiagonalBlock + 2 * a.span + 1) * 4;
+  const bool together = bias_blocks > 0 && std::max(lds, bias_lds) * attn_keys_each<T, D>() <= 160 * 1024;
   a.bias_from = (int)blocks;
   if (blocks + (together ? bias_blocks : 0) > 0 &&
       !launch(attention_dkv_kernel<T, D, BIAS>, blocks + (together ? bias_blocks : 0), together ? std::max(lds, bias_lds) : lds, a, stream))

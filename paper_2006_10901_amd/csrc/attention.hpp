@@ -177,12 +177,14 @@ template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnSt
 };
 
 // Rows of D numbers of TERMS fp16 terms each, the first terms of all, then the second.  In LDS 16 bytes apart from a multiple of the
-// banks: lanes that read 16 bytes of 32 rows meet no conflict.
-template <int D, int TERMS> struct AttnTile {
-  static constexpr int kBytes = D * TERMS * 2, kPitch = kBytes + 16, kSteps = D / 16;
-  // Two tiles (K and V, or Q and dO) at a time, in two sets where two workgroups then fit a compute unit: one is written while the other
-  // is read, and the workgroup meets once per tile.
-  static constexpr int kPair = 2 * kAttnTile * kPitch, kSets = 2 * kPair <= 72 * 1024 ? 2 : 1;
+// banks: lanes that read 16 bytes of 32 rows meet no conflict.  The reads that transpose take 64 bytes of four rows at a time, which then
+// meet in fours where a row is a multiple of the banks: in twos if it is 48 bytes apart from it, for which kernels of EACH = 1 workgroup
+// to a compute unit have room (128 columns, us: dQ in fp32 114 -> 112, dK and dV 142 -> 138, in fp16 127 -> 122).
+template <int D, int TERMS, int EACH = 2> struct AttnTile {
+  static constexpr int kBytes = D * TERMS * 2, kPitch = kBytes + (EACH == 1 && kBytes % 256 == 0 ? 48 : 16), kSteps = D / 16;
+  // Two tiles (K and V, or Q and dO) at a time, in two sets where two workgroups then fit a compute unit (at 128 columns in fp32 one: their
+  // registers let no more in; dK and dV 138 -> 134 us): one is written while the other is read, and the workgroup meets once per tile.
+  static constexpr int kPair = 2 * kAttnTile * kPitch, kSets = 2 * kPair <= (D == 128 ? 144 : 72) * 1024 ? 2 : 1;
   // A tile that is only read by the reads that transpose (V in the forward pass), 64 bytes of four rows at a time: an odd multiple of
   // 64 bytes puts those into all 64 banks, where 16 bytes past a multiple of 256 lets four rows meet in one.
   static constexpr int kPitchT = ((kBytes + 63) / 64 | 1) * 64;
@@ -212,9 +214,9 @@ template <int D, int TERMS> struct AttnOwn {
 };
 
 // X += (32 rows of the tile) (own)^T
-template <int D, int TERMS>
+template <int PITCH, int D, int TERMS>
 __device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const AttnOwn<D, TERMS>& own, int lane) {
-  const char* row = lds + (lane & 31) * AttnTile<D, TERMS>::kPitch + (lane >> 5) * 16;
+  const char* row = lds + (lane & 31) * PITCH + (lane >> 5) * 16;
   f16x8 a[TERMS][D / 16];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s)
@@ -240,7 +242,7 @@ __device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const A
 }
 
 // acc (D x 32, blocks of 32) += (32 rows of the tile)^T X
-template <int D, int TERMS, int PITCH = AttnTile<D, TERMS>::kPitch>
+template <int PITCH, int D, int TERMS>
 __device__ __forceinline__ void attn_product_t(f32x16 (&acc)[D / 32], const char* lds, const f32x16& x, int lane) {
   typedef __attribute__((address_space(3))) s16x4* LdsPtr;
   typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -328,6 +330,9 @@ __device__ __forceinline__ int attn_position(const AttnArgs& a, int batch) {
 }
 
 template <typename T> constexpr int attn_terms() { return sizeof(T) == 4 ? 2 : 1; }
+// How many workgroups of the panel kernels a compute unit holds: those of queries, and those of keys.
+template <typename T, int D> constexpr int attn_queries_each() { return D * attn_terms<T>() <= 128 ? 2 : 1; }
+template <typename T, int D> constexpr int attn_keys_each() { return D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1; }
 
 // How many of its states a sequence has.
 __device__ __forceinline__ int attn_seen(const AttnArgs& a, int batch) { return a.lengths ? min(max(a.lengths[batch], 0), a.k) : a.k; }

@@ -119,10 +119,10 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
 // Two workgroups to a compute unit, with 256 registers a thread, where that spills few of them (us, one -> two: fp16, 128 columns, 2 x 8 heads of
 // 2048 x 2048 99 -> 74; fp32, 64 columns, 8 heads of 4096 x 4096 270 -> 207; but fp32 96 and 128 columns 93 -> 149 and 121 -> 237).
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void attention_dq_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
   constexpr bool kSums = attn_row_sums<T, BIAS>();
-  using Tile = AttnTile<D, kTerms>;
+  using Tile = AttnTile<D, kTerms, attn_queries_each<T, D>()>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);
 
@@ -213,8 +213,8 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
 #pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         f32x16 x = {}, y = {};
-        attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
-        attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+        attn_product<Tile::kPitch>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+        attn_product<Tile::kPitch>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
         weigh(x, key0 + 32 * b - (position + wave_row));
         const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
@@ -232,8 +232,8 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     for (int b = 0; b < 2; ++b) {
       const int near = key0 + 32 * b - (position + wave_row);   // relative position of the block's first key and first query
       f32x16 x = {}, y = {};
-      attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
-      attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+      attn_product<Tile::kPitch>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+      attn_product<Tile::kPitch>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
       __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
       const bool far = weigh(x, near);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
         }
       }
       if (ds_scale.fit(x, acc, ds_scale.factor)) to_ds = own.to_dp * ds_scale.factor, delta_ds = delta * ds_scale.factor, from_ds = 1.f / ds_scale.factor;
-      attn_product_t<D, kTerms>(acc, lds_k + b * 32 * Tile::kPitch, x, lane);
+      attn_product_t<Tile::kPitch, D, kTerms>(acc, lds_k + b * 32 * Tile::kPitch, x, lane);
       __builtin_amdgcn_s_setprio(0);
     }
   }
@@ -360,7 +360,7 @@ __device__ __forceinline__ void attn_sum_diagonals(const f32x16& x, float* block
 template <typename T, int D>
 __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   constexpr int kTerms = attn_terms<T>();
-  using Tile = AttnTile<D, kTerms>;
+  using Tile = AttnTile<D, kTerms, attn_keys_each<T, D>()>;
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kPair);
   float* lds_blocks = lds_bias + (attn_bias_entries(a.span) + 3) / 4 * 4;
   float* lds_sums = lds_blocks + kAttnWaves * kAttnDiagonalBlock;
@@ -426,8 +426,8 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
       const int near = key0 + 32 * b - (position + wave_row);
       if (attn_far(near, a.span)) continue;
       f32x16 x = {}, y = {};
-      attn_product<D, kTerms>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
-      attn_product<D, kTerms>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
+      attn_product<Tile::kPitch>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
+      attn_product<Tile::kPitch>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
       own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
@@ -456,11 +456,10 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
 
 // dK and dV, by panels of 128 keys: a wave has 32 of them, tiles of 64 queries, of every head that shares the keys, are shared by the waves.
 // Two workgroups to a compute unit as for dQ (fp32, 64 columns 369 -> 292 us, fp16 96 106 -> 98), but not at 128 columns (fp16 143 -> 235).
-template <typename T, int D> constexpr int attn_dkv_each() { return D < 128 && D * attn_terms<T>() <= 128 ? 2 : 1; }
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, (attn_dkv_each<T, D>())) void attention_dkv_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
-  using Tile = AttnTile<D, kTerms>;
+  using Tile = AttnTile<D, kTerms, attn_keys_each<T, D>()>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   if (BIAS && (int)blockIdx.x >= a.bias_from) {
     attn_dbias<T, D>(a, lds_raw);
@@ -571,8 +570,8 @@ __global__ __launch_bounds__(256, (attn_dkv_each<T, D>())) void attention_dkv_ke
     for (int b = 0; b < 2; ++b) {
       const int near = wave_key - (position + row0 + 32 * b);
       f32x16 x = {}, y = {};
-      attn_product<D, kTerms>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
-      attn_product<D, kTerms>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
+      attn_product<Tile::kPitch>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
+      attn_product<Tile::kPitch>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
       __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
       const bool far = BIAS && attn_far(near, a.span) && fabsf(near > 0 ? high : low) < kAttnLargeBias;
       if (!BIAS || far) {
@@ -606,9 +605,9 @@ __global__ __launch_bounds__(256, (attn_dkv_each<T, D>())) void attention_dkv_ke
       const float* deltas = lds_delta + b * 32 + half * 4;
 #pragma unroll
       for (int r = 0; r < 16; ++r) y[r] = x[r] * __builtin_fmaf(y[r], to_dp, -deltas[8 * (r / 4) + r % 4]);
-      attn_product_t<D, kTerms>(dv, lds_g + b * 32 * Tile::kPitch, x, lane);
+      attn_product_t<Tile::kPitch, D, kTerms>(dv, lds_g + b * 32 * Tile::kPitch, x, lane);
       if (!ds_scale.fit(y, dk, 1.f)) y *= ds_scale.factor;
-      attn_product_t<D, kTerms>(dk, lds_q + b * 32 * Tile::kPitch, y, lane);
+      attn_product_t<Tile::kPitch, D, kTerms>(dk, lds_q + b * 32 * Tile::kPitch, y, lane);
       __builtin_amdgcn_s_setprio(0);
     }
   }

@@ -7,9 +7,9 @@ namespace spdl {
 
 // Panels of 128 queries: a wave has 32 of them, tiles of 64 keys are shared by the four waves.
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void attention_forward_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_forward_kernel(const AttnArgs a) {
   constexpr int kTerms = attn_terms<T>();
-  using Tile = AttnTile<D, kTerms>;
+  using Tile = AttnTile<D, kTerms, attn_queries_each<T, D>()>;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   constexpr int kPair = kAttnTile * (Tile::kPitch + Tile::kPitchT);
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kSets * kPair);
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
     if (wave_row >= a.m || !__any(word != 0)) continue;   // none of the wave's queries sees the tile
     f32x16 x[2] = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) attn_product<D, kTerms>(x[b], lds_k + b * 32 * Tile::kPitch, q, lane);
+    for (int b = 0; b < 2; ++b) attn_product<Tile::kPitch>(x[b], lds_k + b * 32 * Tile::kPitch, q, lane);
     AttnScores how = {scale, false, 0.f};
     if (BIAS) {
       const int near = key0 - (position + wave_row);     // relative position of the tile's first key and the wave's first query
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256, D * attn_terms<T>() <= 128 ? 2 : 1) void atten
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       attn_weights(x[b], run, to);
-      attn_product_t<D, kTerms, Tile::kPitchT>(acc, lds_v + b * 32 * Tile::kPitchT, x[b], lane);
+      attn_product_t<Tile::kPitchT, D, kTerms>(acc, lds_v + b * 32 * Tile::kPitchT, x[b], lane);
     }
     __builtin_amdgcn_s_setprio(0);
   }
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attention_tokens_kernel(
     word &= attn_low_bits(seen - key0);
     if (!__any(word != 0)) continue;
     f32x16 x[1] = {};
-    attn_product<D, 1>(x[0], lds_k, q, lane);
+    attn_product<Tile::kPitch>(x[0], lds_k, q, lane);
     if (BIAS && (key0 - (first + a.m - 1) >= a.span || key0 + 31 - first <= -a.span)) {
       attn_add_constant(x[0], scale, key0 > first ? high : low);      // each lane's own head
     } else if (BIAS) {
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attention_tokens_kernel(
     }
     if (__any(word != ~0u)) attn_hide(x[0], word, half);
     attn_weights(x[0], run, attn_softmax_step<D, 1>(x, run, acc, AttnScores{scale, BIAS, 0.f}));
-    attn_product_t<D, 1>(acc, lds_v, x[0], lane);
+    attn_product_t<Tile::kPitch, D, 1>(acc, lds_v, x[0], lane);
   }
 
   // the four waves' parts, in LDS: [4][32][D + 1] sums, [4][32][2] statistics
