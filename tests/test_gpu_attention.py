@@ -76,6 +76,14 @@ def test_bias(dtype, buckets, span, both, m, k, positions):
          seed=span).check(what=f"{dtype} {buckets} {span} {m}x{k}")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("heads,kv_heads,m,k", [(40, 1, 1, 400), (40, 1, 5, 90), (2, 2, 150, 2500)])
+def test_the_largest_bias(dtype, d, heads, kv_heads, m, k):
+    """What most LDS is taken for: 2049 relative positions and 128 buckets beside tiles of every width."""
+    Case(dtype, heads=heads, kv_heads=kv_heads, m=m, k=k, d=d, buckets=128, span=1024, positions=[k // 2], seed=d).check(what=f"{dtype} {d} {m}x{k}")
+
+
 @pytest.mark.parametrize("m,k,lengths,mask,buckets", [(300, 2, None, None, 0), (300, 5, None, None, 16), (300, 20, None, None, 0), (100, 700, [3, 40], None, 16),
                                                       (20, 700, [64, 2], None, 0), (64, 64, None, causal, 0), (128, 500, None, causal, 16)])
 def test_gradients_of_rows_that_see_few_keys_in_half_precision(m, k, lengths, mask, buckets):
