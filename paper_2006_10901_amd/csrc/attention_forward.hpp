@@ -719,6 +719,39 @@ __device__ __forceinline__ float attn_largest(float most, const f32x4& v) {
   }
   return most;
 }
+// Of rows [begin, end), by 256 threads, AHEAD pieces of 16 bytes each at a time (behind the last row that one again); no piece crosses a
+// row's end, the last one of a row may overlap the one before.
+template <int AHEAD>
+__device__ __forceinline__ float attn_largest_of(const AttnOperands& o, const AttnOperand& x, int batch, int kv_head, int begin, int end) {
+  const int pieces = (o.d + 3) / 4, row_step = 256 / pieces, piece_step = 256 % pieces;
+  const float* base = static_cast<const float*>(x.from) + batch * x.s.batch + (int64_t)kv_head * x.group * x.s.head;
+  int r = begin + threadIdx.x / pieces, c = threadIdx.x % pieces;
+  auto next = [&]() {
+    const int at = min(r, end - 1), g = x.group > 1 ? (unsigned)at / (unsigned)x.rows : 0;
+    const float* row = base + g * x.s.head + (int64_t)(at - g * x.rows) * x.s.row + 4 * c;
+    r += row_step;
+    c += piece_step;
+    if (c >= pieces) c -= pieces, ++r;
+    return row;
+  };
+  float most = 0.f;
+  while (r < end) {
+    f32x4 v[AHEAD];
+    if (o.d >= 4) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int back = max(4 * c + 4 - o.d, 0);
+        v[i] = *reinterpret_cast<const AttnPiece<float>::Any*>(next() - back);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) v[i] = attn_load_piece<float>(next(), 0, o.d);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) most = attn_largest(most, v[i]);
+  }
+  return most;
+}
 __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperands o) {
   __shared__ float waves[4];
   int64_t id = blockIdx.x;
@@ -728,13 +761,8 @@ __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperan
   id /= o.count;
   const int kv_head = (int)(id % o.kv_heads), batch = (int)(id / o.kv_heads);
   const AttnOperand& x = o.of[which];
-  const int64_t rows = attn_operand_rows(o, x, batch), begin = rows * part / o.parts, end = rows * (part + 1) / o.parts;
-  const int pieces = (o.d + 3) / 4;
-  float most = 0.f;
-  for (int64_t at = begin * pieces + threadIdx.x; at < end * pieces; at += 256) {
-    const int64_t r = at / pieces;
-    most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, r), (int)(at - r * pieces) * 4, o.d));
-  }
+  const int64_t rows = attn_operand_rows(o, x, batch);
+  float most = attn_largest_of<4>(o, x, batch, kv_head, (int)(rows * part / o.parts), (int)(rows * (part + 1) / o.parts));
 #pragma unroll
   for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
@@ -767,12 +795,7 @@ __global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands
       if (o.most) {
         most = lane < o.parts ? o.most[(bh * 4 + which) * o.parts + lane] : 0.f;
       } else {                                            // few numbers: every workgroup looks at all of them
-        const int pieces = (o.d + 3) / 4;
-#pragma unroll 4
-        for (int64_t at = threadIdx.x; at < rows * pieces; at += 256) {
-          const int64_t row = at / pieces;
-          most = attn_largest(most, attn_load_piece<float>(attn_operand_row<float>(x, batch, kv_head, row), (int)(at - row * pieces) * 4, o.d));
-        }
+        most = attn_largest_of<8>(o, x, batch, kv_head, 0, (int)rows);
       }
 #pragma unroll
       for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
