@@ -39,6 +39,7 @@ struct Entry {
 // The C entry points' parameter classes before the stream: i = int, f = float, p = pointer.
 const char* const kForms[] = {"iiiipppppp", "iiiippppp", "iiiippppppip", "iippfp", "iippp", "iiippp", "ppppppppppppl", "pppppppppppppppppl"};
 constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
+constexpr int kAttentionForms = 5;   // from which one on they are attention's: the mask, forward, backward
 
 // Raised through a callback, so that the exception class lives in Python.
 PyObject* g_raise_status = nullptr;
@@ -223,9 +224,9 @@ PyObject* call_entry(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
         problem = static_cast<const spdl_attention_problem*>(p[np++]);
       } else if (!as_pointer(args[a], arg, &p[np++])) {
         return nullptr;
-      } else if (problem && args[a] != Py_None) {
+      } else if (e.form >= kAttentionForms && args[a] != Py_None) {
         const at::Tensor& t = THPVariable_Unpack(args[a]);
-        if (arg.strided ? !fits_problem(t, arg, *problem) : !long_enough(t, arg, *problem)) return nullptr;
+        if (problem && (arg.strided ? !fits_problem(t, arg, *problem) : !long_enough(t, arg, *problem))) return nullptr;
         if (arg.kind == 'W') bytes = t.numel();
         if (!guard.current_device()) {
           guard.set_index(t.device().index());
