@@ -240,7 +240,7 @@ bool launch_forward(const Plan& x, AttnArgs a, char* w, hipStream_t stream) {
   }
   if (!prepare_operands<T, D>(x, a, w, false, stream)) return false;
   using Tile = AttnTile<D, attn_terms<T>(), attn_queries_each<T, D>()>;
-  const int lds = Tile::kSets * kAttnTile * (Tile::kPitch + Tile::kPitchT) + (BIAS ? attn_bias_entries(a.span) * 4 : 0);
+  const int lds = Tile::kSets * kAttnTile * (Tile::kPitch + Tile::kPitchT) + (BIAS ? attn_bias_entries(a.span, kAttnPad) * 4 : 0);
   a.again = reinterpret_cast<unsigned*>(w + x.forward_again);
   if (!launch(attention_forward_kernel<T, D, BIAS>, x.forward_blocks * a.splits, lds, a, stream)) return false;
   return !a.mask || launch(attention_forward_again_kernel<T>, x.forward_blocks * a.splits, 0, a, stream);
@@ -250,7 +250,7 @@ template <typename T, int D, bool BIAS>
 bool launch_backward(const Plan& x, AttnArgs a, char* w, void* dtable, hipStream_t stream) {
   using Queries = AttnTile<D, attn_terms<T>(), attn_queries_each<T, D>()>;
   using Keys = AttnTile<D, attn_terms<T>(), attn_keys_each<T, D>()>;
-  const int bias = BIAS ? attn_bias_entries(a.span) * 4 : 0;
+  const int bias = BIAS ? attn_bias_entries(a.span, kAttnPadBlock) * 4 : 0;
   const int64_t pieces = up(a.d, 4);
   a.part = reinterpret_cast<float*>(w + x.part);
   a.again = reinterpret_cast<unsigned*>(w + x.backward_again);

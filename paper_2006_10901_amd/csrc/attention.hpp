@@ -115,6 +115,18 @@ __device__ __forceinline__ typename AttnPiece<T>::Type attn_load_whole_piece(con
   return *reinterpret_cast<const typename AttnPiece<T>::Any*>(row + min(c0, d - 16 / (int)sizeof(T)));
 }
 
+// Four neighbouring elements of a row of d, of the parts s, s + step .. that splits left (behind the last one that again): asked for together.
+__device__ __forceinline__ void attn_load_parts(f32x4 (&v)[4], const float* part, int splits, int s, int step, int64_t rows, int64_t flat, int c, int d) {
+  auto row = [&](int u) { return part + (min(s + u * step, splits - 1) * rows + flat) * d; };
+  if (d % 4 == 0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = attn_load_whole_piece<float>(row(u), c, d);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = attn_load_piece<float>(row(u), c, d);
+  }
+}
+
 // A tile on its way from memory to LDS, requested a tile ahead into registers, then written: ROWS rows of BYTES bytes, PITCH apart.
 template <typename T, int ROWS, int BYTES, int PITCH, int THREADS> struct AttnStage {
   using Piece = typename AttnPiece<T>::Type;
@@ -311,15 +323,15 @@ __device__ __forceinline__ void attn_store_rows(T* row, bool valid, const f32x16
 
 __device__ __forceinline__ unsigned attn_low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// The bias of one head by relative position, in LDS: entry x is that of relative position x - span - kAttnPad, clamped, so that a
-// pair of tiles that comes near the clamped ends needs no clamping of its own.
-constexpr int kAttnPad = 96;
-__host__ __device__ __forceinline__ int attn_bias_entries(int span) { return 2 * span + 1 + 2 * kAttnPad; }
-template <typename T>
+// The bias of one head by relative position, in LDS: entry x is that of relative position x - span - PAD, clamped, so that tiles that
+// come near the clamped ends need no clamping of their own: 32 queries and 64 keys (forward) or 32 (backward).
+constexpr int kAttnPad = 96, kAttnPadBlock = 64;
+__host__ __device__ __forceinline__ int attn_bias_entries(int span, int pad) { return 2 * span + 1 + 2 * pad; }
+template <typename T, int PAD>
 __device__ __forceinline__ void attn_fill_bias(float* lds, const AttnArgs& a, int head, int tid, int threads) {
   const T* row = static_cast<const T*>(a.table) + (int64_t)head * a.buckets;
-  for (int x = tid; x < attn_bias_entries(a.span); x += threads) {
-    const int b = a.bucket_of[min(max(x - kAttnPad, 0), 2 * a.span)];
+  for (int x = tid; x < attn_bias_entries(a.span, PAD); x += threads) {
+    const int b = a.bucket_of[min(max(x - PAD, 0), 2 * a.span)];
     lds[x] = (float)row[min(max(b, 0), a.buckets - 1)];
   }
 }

@@ -70,13 +70,21 @@ __device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat,
     a.ends[2 * flat + 1] = (float)(weight * (s.high - more * s.high_p));
   }
 }
-template <bool BIAS> __device__ __forceinline__ AttnRowSums attn_row_sums_of(const AttnArgs& a, int64_t flat, bool ends) {
+template <bool BIAS> __device__ __forceinline__ AttnRowSums attn_row_sums_of(const AttnArgs& a, int64_t flat) {
   const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   AttnRowSums s = {};
-  for (int i = 0; i < a.splits; ++i) {
-    const double* from = a.row_sums + (i * rows + flat) * kAttnRowSums;
-    s.ds += from[0], s.p += from[1];
-    if (BIAS && ends) s.low += from[2], s.low_p += from[3], s.high += from[4], s.high_p += from[5];
+  for (int i0 = 0; i0 < a.splits; i0 += 4) {             // four parts asked for at a time, behind the last one that again
+    double v[4][kAttnRowSums];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int x = 0; x < (BIAS ? kAttnRowSums : 2); ++x) v[u][x] = a.row_sums[(min(i0 + u, a.splits - 1) * rows + flat) * kAttnRowSums + x];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u >= a.splits) break;
+      s.ds += v[u][0], s.p += v[u][1];
+      if (BIAS) s.low += v[u][2], s.low_p += v[u][3], s.high += v[u][4], s.high_p += v[u][5];
+    }
   }
   return s;
 }
@@ -163,7 +171,7 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
   AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   int position = 0;
   if (BIAS) {
-    attn_fill_bias<T>(lds_bias, a, head, tid, 256);
+    attn_fill_bias<T, kAttnPadBlock>(lds_bias, a, head, tid, 256);
     position = attn_position(a, batch);
   }
   AttnRowSums sums = {};
@@ -176,8 +184,8 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
   auto weigh = [&](f32x16& x, int near) {
     const bool far = BIAS && attn_far(near, a.span);
     if (!BIAS) own.weights(x, 0.f);
-    else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPad : kAttnPad]);
-    else own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+    else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPadBlock : kAttnPadBlock]);
+    else own.weights(x, lds_bias + kAttnPadBlock + a.span + near - (lane & 31) + 4 * half);
     return far;
   };
   float to_ds = own.to_dp, delta_ds = delta, from_ds = 1.f;   // what makes dS, taken times the factor of ds_scale
@@ -362,7 +370,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   constexpr int kTerms = attn_terms<T>();
   using Tile = AttnTile<D, kTerms, attn_keys_each<T, D>()>;
   float* lds_bias = reinterpret_cast<float*>(lds_raw + Tile::kPair);
-  float* lds_blocks = lds_bias + (attn_bias_entries(a.span) + 3) / 4 * 4;
+  float* lds_blocks = lds_bias + (attn_bias_entries(a.span, kAttnPadBlock) + 3) / 4 * 4;
   float* lds_sums = lds_blocks + kAttnWaves * kAttnDiagonalBlock;
   const int n = 2 * a.span + 1;
 
@@ -383,7 +391,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
   AttnQueries<T, D, true> own;
   own.load(a, at, f, row, valid, half);
-  attn_fill_bias<T>(lds_bias, a, head, tid, 256);
+  attn_fill_bias<T, kAttnPadBlock>(lds_bias, a, head, tid, 256);
   float* sums = lds_sums + wave * n;
   float* block = lds_blocks + wave * kAttnDiagonalBlock;
   for (int x = lane; x < n; x += 64) sums[x] = 0.f;
@@ -428,7 +436,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
       f32x16 x = {}, y = {};
       attn_product<Tile::kPitch>(x, lds_k + b * 32 * Tile::kPitch, own.q, lane);
       attn_product<Tile::kPitch>(y, lds_v + b * 32 * Tile::kPitch, own.g, lane);
-      own.weights(x, lds_bias + kAttnPad + a.span + near - (lane & 31) + 4 * half);
+      own.weights(x, lds_bias + kAttnPadBlock + a.span + near - (lane & 31) + 4 * half);
       const unsigned w = (unsigned)(word >> (32 * b)) >> (4 * half);
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = attn_select(w, r, x[r] * weight * __builtin_fmaf(y[r], own.to_dp, -delta), 0.f);
@@ -544,10 +552,10 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     const uint64_t word = valid ? word_next : 0ull;
     if (BIAS && h != bias_head) {
       __syncthreads();                                    // the head before may still be at work
-      attn_fill_bias<T>(lds_bias, a, kv_head * a.group + h, tid, 256);
+      attn_fill_bias<T, kAttnPadBlock>(lds_bias, a, kv_head * a.group + h, tid, 256);
       __syncthreads();
       bias_head = h;
-      low = lds_bias[kAttnPad], high = lds_bias[2 * a.span + kAttnPad];
+      low = lds_bias[kAttnPadBlock], high = lds_bias[2 * a.span + kAttnPadBlock];
     }
     if (tid < 64) {
       // rows that see nothing, and those behind the last, have no weights
@@ -584,7 +592,7 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
         const float* l = lds_lse + b * 32 + half * 4;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float bias = lds_bias[kAttnPad + min(max(rel - (8 * (r / 4) + r % 4), 0), 2 * a.span)];
+          const float bias = lds_bias[kAttnPadBlock + min(max(rel - (8 * (r / 4) + r % 4), 0), 2 * a.span)];
           x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(x[r], scale, bias) - l[8 * (r / 4) + r % 4], kLog2e, kOffset));
         }
       }
@@ -660,8 +668,13 @@ template <typename T>
 __device__ __forceinline__ void attn_add_parts(int splits, int64_t rows, int heads, int per_head, int d, const float* part, int64_t flat, int c, float weight,
                                                const AttnSum& x) {
   f32x4 s = {};
-#pragma unroll 4
-  for (int i = 0; i < splits; ++i) s += attn_load_piece<float>(part + (i * rows + flat) * d, c, d);
+  for (int i0 = 0; i0 < splits; i0 += 4) {
+    f32x4 v[4];
+    attn_load_parts(v, part, splits, i0, 1, rows, flat, c, d);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u < splits) s += v[u];
+  }
   s *= weight;
   const int64_t bh = flat / per_head;
   T* row = static_cast<T*>(x.out) + bh / heads * x.to.batch + bh % heads * x.to.head + (flat % per_head) * x.to.row;
@@ -679,7 +692,7 @@ __global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a)
   const bool first = at % pieces == 0;
   float weight = 1.f;
   if (SUMS && (sizeof(T) == 4 || first)) {
-    const AttnRowSums s = attn_row_sums_of<BIAS>(a, flat, first);
+    const AttnRowSums s = attn_row_sums_of<BIAS>(a, flat);
     weight = (float)attn_row_weight<T>(s);
     if (first) attn_finish_row<T, BIAS>(a, flat, a.delta[flat], s);
   }
@@ -698,8 +711,14 @@ __device__ __forceinline__ void attn_dtable(const AttnArgs& a, int head, int par
     const int group = at / n, x = at - group * n, end = (int)((int64_t)parts * (group + 1) / groups);
     const int bucket = a.bucket_of[x];
     double s = 0.;
-#pragma unroll 16
-    for (int i = (int)((int64_t)parts * group / groups); i < end; ++i) s += from[(int64_t)i * n + x];
+    for (int i0 = (int)((int64_t)parts * group / groups); i0 < end; i0 += 16) {   // sixteen asked for at a time
+      float v[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) v[u] = from[(int64_t)min(i0 + u, end - 1) * n + x];
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        if (i0 + u < end) s += v[u];
+    }
     sums[at] = s;
     if (group == 0) buckets[x] = min(max(bucket, 0), a.buckets - 1);
   }

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_fo
   AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
   int position = 0;
   if (BIAS) {
-    attn_fill_bias<T>(lds_bias, a, head, tid, 256);
+    attn_fill_bias<T, kAttnPad>(lds_bias, a, head, tid, 256);
     position = attn_position(a, batch);
   }
 
@@ -613,11 +613,15 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a) {
   for (int c0 = 0; c0 < a.d; c0 += 64) {                  // every lane stays: the others read its weight
     const int c = c0 + lane % 16 * 4;
     f32x4 value = {};
-    for (int s0 = 0; s0 < a.splits; s0 += kTurns) {
-      const int s = min(s0 + turn, a.splits - 1);
-      const float there = __shfl(weight, s, LANES), w = s0 + turn < a.splits ? there : 0.f;
-      const f32x4 v = attn_load_piece<float>(a.part + (s * rows + flat) * a.d, c, a.d);
-      if (w != 0.f) value += w * v;
+    for (int s0 = 0; s0 < a.splits; s0 += 4 * kTurns) {   // four parts asked for at a time
+      f32x4 v[4];
+      attn_load_parts(v, a.part, a.splits, s0 + turn, kTurns, rows, flat, c, a.d);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = s0 + turn + u * kTurns;
+        const float there = __shfl(weight, min(s, a.splits - 1), LANES), w = s < a.splits ? there : 0.f;
+        if (w != 0.f) value += w * v[u];
+      }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
