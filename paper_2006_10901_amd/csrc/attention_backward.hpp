@@ -700,7 +700,7 @@ __global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a)
 }
 
 // dtable of one head: the panels' sums by relative position (runs of panels by as many groups of threads as 1024 allow, added up in their
-// order), then those of a bucket, in ascending position, eight threads to a bucket.
+// order), then those of a bucket, in ascending position, 8 to 64 threads to a bucket.
 template <typename T>
 __device__ __forceinline__ void attn_dtable(const AttnArgs& a, int head, int parts, T* dtable, char* lds_raw) {
   const int n = 2 * a.span + 1, groups = n < 1024 ? 1024 / n : 1;
@@ -729,13 +729,12 @@ __device__ __forceinline__ void attn_dtable(const AttnArgs& a, int head, int par
     sums[x] = s;
   }
   __syncthreads();
-  const int b = threadIdx.x >> 3, eighth = threadIdx.x & 7;
+  const int each = a.buckets <= 16 ? 64 : a.buckets <= 32 ? 32 : a.buckets <= 64 ? 16 : 8, b = threadIdx.x / each, part = threadIdx.x % each;
   double s = 0.;
 #pragma unroll 4
-  for (int x = n * eighth / 8; x < n * (eighth + 1) / 8; ++x) s += buckets[x] == b ? sums[x] : 0.;
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o);
-  if (eighth == 0 && b < a.buckets) dtable[(int64_t)head * a.buckets + b] = (T)s;
+  for (int x = n * part / each; x < n * (part + 1) / each; ++x) s += buckets[x] == b ? sums[x] : 0.;
+  for (int o = 1; o < each; o <<= 1) s += __shfl_xor(s, o);
+  if (part == 0 && b < a.buckets) dtable[(int64_t)head * a.buckets + b] = (T)s;
 }
 
 // What is left when the panels are done: dtable, a workgroup per head (`tables` of them), and dK and dV added up where they were split.
