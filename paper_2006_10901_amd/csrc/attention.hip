@@ -93,11 +93,12 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   if (x.copied) {
     x.most = take(terms, (int64_t)p.batch * p.kv_heads * 4 * x.most_parts);
     x.factors = take(terms, (int64_t)p.batch * p.kv_heads * 4);
-    x.q16 = take(terms, x.rows * numbers);
     x.k16 = take(terms, x.kv_rows * numbers);
     x.v16 = take(terms, x.kv_rows * numbers);
+    end = terms;
+    x.q16 = take(terms, x.rows * numbers);
   }
-  end = x.token ? 0 : terms;
+  end = x.token ? 0 : elem_bytes == 4 ? end : terms;      // the forward pass in single precision needs no terms of Q
   if (x.forward_splits > 1) {
     x.forward_part = take(end, x.forward_splits * x.rows * p.d);
     x.part_sum = take(end, 2 * x.forward_splits * x.rows);
@@ -197,7 +198,9 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
     terms = at;
     strides = {(int64_t)a.kv_heads * group * rows * kWidth, (int64_t)rows * kWidth, kWidth};
   };
-  operand(a.Q, a.q, x.q16, a.group, a.m, 0, a.q16, a.q16s);
+  const bool queries = backward || sizeof(T) == 2;        // (the forward kernel takes Q's numbers as they are)
+  o.first = queries ? 0 : 1;
+  if (queries) operand(a.Q, a.q, x.q16, a.group, a.m, 0, a.q16, a.q16s);
   operand(a.K, a.kk, x.k16, 1, a.k, 1, a.k16, a.k16s);
   operand(a.V, a.v, x.v16, 1, a.k, 1, a.v16, a.v16s);
   if (backward) operand(a.dO, a.dout, x.g16, a.group, a.m, 0, a.g16, a.g16s);
@@ -207,13 +210,15 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
   o.most = reinterpret_cast<float*>(w + x.most), o.factors = reinterpret_cast<float*>(w + x.factors);
   const int64_t each = (int64_t)a.batch * a.kv_heads * o.count;
   // of few numbers the workgroups that make the terms find the largest themselves, which saves a launch
-  if (std::max<int64_t>((int64_t)a.group * a.m, a.k) * a.d <= 32768) {
+  const int64_t rows = std::max<int64_t>(queries ? (int64_t)a.group * a.m : 0, a.k);
+  if (rows * a.d <= 32768) {
     o.most = nullptr;
   } else if (sizeof(T) == 4) {
     attention_largest_kernel<<<dim3((unsigned)(each * o.parts)), dim3(256), 0, stream>>>(o);
     if (hipGetLastError() != hipSuccess) return false;
   }
-  const int64_t blocks = up(std::max<int64_t>((int64_t)a.group * a.m, a.k), 256 / (D / 8));
+  if (rows == 0) return true;
+  const int64_t blocks = up(rows, 256 / (D / 8));
   attention_terms_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)std::min<int64_t>(each, 32768)), dim3(256), 0, stream>>>(o, (int)each);
   return hipGetLastError() == hipSuccess;
 }

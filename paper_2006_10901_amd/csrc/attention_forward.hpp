@@ -25,11 +25,15 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_fo
 
   const _Float16* K = a.k16 + batch * a.k16s.batch + kv_head * a.k16s.head;
   const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
-  AttnOwn<D, kTerms> q;
-  q.load(a.q16 + batch * a.q16s.batch + head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
-  if (a.scale < 0.f) q.negate();                         // so that the largest score is the largest product
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
-  const float scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
+  AttnOwn<D, kTerms> q;
+  float to_score = f.k;
+  if constexpr (kTerms == 2)
+    to_score *= q.load_numbers(static_cast<const float*>(a.Q) + batch * a.q.batch + head * a.q.head, row * a.q.row, valid, a.d, half);
+  else
+    q.load(a.q16 + batch * a.q16s.batch + head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
+  if (a.scale < 0.f) q.negate();                         // so that the largest score is the largest product
+  const float scale = fmaxf(fabsf(a.scale) * to_score, kAttnLeastScale);
 
   const MaskLayout lay(a.m, a.k);
   AttnSeenTiles tiles(a.mask, lay.row_tiles, lay.tj, lay.ti, first_row);
@@ -702,7 +706,7 @@ struct AttnOperand {
 };
 struct AttnOperands {
   AttnOperand of[4];
-  int count, batch, kv_heads, d, k, parts;
+  int count, first, batch, kv_heads, d, k, parts;   // first: of Q, K, V, dO
   const int* lengths;
   float *most, *factors;    // [batch * kv_heads][4][parts], [batch * kv_heads][4]
 };
@@ -714,14 +718,6 @@ template <typename T>
 __device__ __forceinline__ const T* attn_operand_row(const AttnOperand& x, int batch, int kv_head, int64_t r) {
   const int g = (int)(r / x.rows);
   return static_cast<const T*>(x.from) + batch * x.s.batch + ((int64_t)kv_head * x.group + g) * x.s.head + (r - (int64_t)g * x.rows) * x.s.row;
-}
-__device__ __forceinline__ float attn_largest(float most, const f32x4& v) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float m = fabsf(v[e]);
-    most = m < __builtin_inff() ? fmaxf(most, m) : most;
-  }
-  return most;
 }
 // Of rows [begin, end), by 256 threads, AHEAD pieces of 16 bytes each at a time (behind the last row that one again); no piece crosses a
 // row's end, the last one of a row may overlap the one before.
@@ -809,9 +805,9 @@ __global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands
         __syncthreads();
         most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
       }
-      const int e = most > 0.f ? min(max(14 - ilogbf(most), -120), 120) : 0;
+      const int e = attn_exponent(most);
       const float factor = ldexpf(1.f, e);
-      if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + which] = ldexpf(1.f, -e);
+      if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + o.first + which] = ldexpf(1.f, -e);
       f16x8 hi = {}, lo = {};
       if (mine && r < rows) {
         const float* row = attn_operand_row<float>(x, batch, kv_head, r);
