@@ -102,8 +102,8 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
     if (a.scale < 0.f) q.negate();
     scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
     to_dp = f.g * f.v;
-    lse = valid ? a.lse[flat] : 0.f;
-    if (lse == -__builtin_inff()) lse = __builtin_inff();  // a row that sees nothing has no weights
+    lse = valid ? a.lse[flat] : -__builtin_inff();
+    if (lse == -__builtin_inff()) lse = __builtin_inff();  // rows that see nothing, and those behind the last, have no weights
   }
   // Products become weights, with one bias for all of them (AttnScores), or each with its own
   __device__ __forceinline__ void weights(f32x16& x, float bias) const {
@@ -425,7 +425,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
     stage_k.store(lds_k, tid);
     stage_v.store(lds_v, tid);
     const int key0 = t * kAttnTile;
-    const uint64_t word = attn_first(word_next, seen - key0);
+    const uint64_t word = valid ? attn_first(word_next, seen - key0) : 0ull;     // (a diagonal's sum takes in lanes behind the last row)
     __syncthreads();
     t = tiles.next(t + 1, end);
     if (t < end) load(t);

@@ -1,0 +1,44 @@
+"""Attention where numbers, lengths and masks meet the ends of what they may be: large biases and scores, Inf and NaN beside rows that
+see nothing and behind a sequence's states, numbers of unequal size in one head."""
+import pytest
+import torch
+
+import paper_2006_10901_amd as spdl
+from tests.attention_util import Case, causal, reference, sparse_rows
+from tests.gpu_util import TOL_F16, TOL_F32
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["f32", "f16"]
+
+
+def step(case):
+    case.prepare()
+    case.forward()
+    case.backward()
+    torch.cuda.synchronize()
+    return {name: t.cpu().double() for name, t in case.results().items()}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,span", [(1, 90, 16), (40, 70, 16), (40, 2050, 128), (130, 200, 0), (33, 40, 40)])
+@pytest.mark.parametrize("lengths", [None, [35, 29]])
+def test_a_large_bias_beside_rows_that_are_not_there(dtype, m, k, span, lengths):
+    """exp(100) is more than fp32 holds: lanes behind the last query, whose products are 0, must not have such weights.
+    Weights count to 2^-39 of a row's largest, dS to 2^-36 of a block's, so that those of exp(-100) are lost: each of the terms that a result adds up, at most
+    2 max(m, k) of them (dtable: m k), may be off by 2^-36 times the most that it multiplies a weight by."""
+    case = Case(dtype, batch=2, heads=3, m=m, k=k, d=32, buckets=8, span=span, lengths=lengths, seed=m)
+    case.table[0] = 100.0
+    case.table[1, ::2] = 100.0
+    got = step(case)
+    want = reference(case.Q, case.K, case.V, case.scale, case.lengths, case.positions, case.seen, case.bucket_of, case.table, case.dO)
+    Q, K, V, dO = (float(t.nan_to_num().abs().max()) for t in (case.Q, case.K, case.V, case.dO))
+    slope = 2 * 32 * dO * V                              # the most that dP - D can be
+    more = {"O": 2 * max(m, k) * V, "dV": 2 * max(m, k) * dO, "dQ": 2 * max(m, k) * case.scale * slope * K, "dK": 2 * max(m, k) * case.scale * slope * Q,
+            "dtable": 2 * m * k * slope}
+    for name, times in more.items():
+        result, S = want[name]
+        off = (got[name] - result).abs()
+        tol, least = (TOL_F16, 2.0 ** -25) if dtype == "f16" else (TOL_F32, 0.0)
+        assert (off <= tol * S + least + 2.0 ** -36 * times).all(), f"{name}: {off.max()}"
+    assert ((got["lse"] - want["lse"][0]).abs() <= 1e-4).all()
