@@ -282,6 +282,13 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
     }
   }
 
+  // a row that sees nothing: its dS of 0 times Inf or NaN of states that its neighbours see is NaN, and so may D be
+  const bool none = own.lse == __builtin_inff();
+  if (none) {
+    delta = 0.f;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) acc[b] = f32x16{};
+  }
   float weight = 1.f;                                    // what the row's P is taken times
   const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   if constexpr (kSums) {
@@ -303,7 +310,7 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
     a.delta[own.flat] = delta;
   }
   if (a.mask) {
-    // (rows whose own numbers are Inf or NaN are right as they are)
+    // (rows whose own numbers are Inf or NaN are right as they are, and so are those that see nothing)
     const unsigned bad = attn_not_finite(acc, false) & (unsigned)__ballot(valid && attn_finite(own.lse) && attn_finite(delta));
     if (lane == 0) a.again[blockIdx.x * kAttnWaves + wave] = bad;
   }

@@ -3,8 +3,7 @@ see nothing and behind a sequence's states, numbers of unequal size in one head.
 import pytest
 import torch
 
-import paper_2006_10901_amd as spdl
-from tests.attention_util import Case, causal, reference, sparse_rows
+from tests.attention_util import Case, reference, sparse_rows
 from tests.gpu_util import TOL_F16, TOL_F32
 
 pytestmark = pytest.mark.gpu
@@ -42,3 +41,30 @@ def test_a_large_bias_beside_rows_that_are_not_there(dtype, m, k, span, lengths)
         tol, least = (TOL_F16, 2.0 ** -25) if dtype == "f16" else (TOL_F32, 0.0)
         assert (off <= tol * S + least + 2.0 ** -36 * times).all(), f"{name}: {off.max()}"
     assert ((got["lse"] - want["lse"][0]).abs() <= 1e-4).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("what", ["K", "V", "Q", "dO"])
+@pytest.mark.parametrize("m,k,bias", [(40, 90, 0), (70, 2050, 0), (70, 2050, 8), (5, 90, 8)])
+def test_rows_that_see_nothing_beside_non_finite_numbers(dtype, value, what, m, k, bias):
+    """Every third row sees nothing: whatever its neighbours see, and whatever stands in its own Q and dO, it gives 0 and adds nothing."""
+    case = Case(dtype, heads=2, m=m, k=k, d=48, mask=sparse_rows, buckets=bias, span=20, seed=m)
+    empty = torch.arange(m) % 3 == 0
+    at = k // 2
+    case.seen[1::3, at] = True                           # neighbours of empty rows see what is put there
+    case.mask = case.build_mask()
+    clean = reference(case.Q, case.K, case.V, case.scale, None, None, case.seen, case.bucket_of, case.table, case.dO)
+    if what in ("K", "V"):
+        getattr(case, what)[0, 1, at] = value
+    else:
+        getattr(case, what)[0, 1, 3] = value             # a row that sees nothing
+    got = step(case)
+    assert (got["O"][0, :, empty] == 0).all() and torch.isneginf(got["lse"][0, :, empty]).all()
+    assert (got["dQ"][0, :, empty] == 0).all()
+    if what in ("Q", "dO"):
+        tol = TOL_F16 if dtype == "f16" else TOL_F32
+        for name in ("O", "dQ", "dK", "dV", "dtable")[: 5 if bias else 4]:
+            want, S = clean[name]
+            assert torch.isfinite(got[name]).all(), name
+            assert ((got[name] - want).abs() <= tol * S + 2.0 ** -25).all(), name
