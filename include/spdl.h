@@ -282,7 +282,8 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  * that keeps them in its range) before they are multiplied, and results are rounded once.  Two calls on the same inputs give the same bits.
  * Inf and NaN: a row that does not see a state, by its mask or the sequence's length, is not touched by what stands there, and neither
  * are gradients; with a mask, rows that such numbers would reach otherwise are formed again one position at a time, at the speed of
- * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.
+ * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.  A bias of -inf is no mask in this sense: the
+ * weight of 0 that it gives, times Inf or NaN, may be NaN in O and in the gradients (a row all of whose scores are -inf still has O = 0 and dQ = 0).
  * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once.  */
 typedef struct { int64_t batch, head, row; } spdl_strides;
 typedef struct {

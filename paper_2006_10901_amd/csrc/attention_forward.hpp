@@ -106,7 +106,11 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_fo
   }
 
   const float total = attn_sum_halves(run.sum);
-  const bool none = total == 0.f;                        // (a sum of NaN is none)
+  const bool none = total == 0.f;                        // (NaN is no such sum); weights of 0 times Inf are NaN
+  if (none) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) acc[b] = f32x16{};
+  }
   const float2 sum = {run.most, total * __builtin_amdgcn_exp2f(-kOffset)};
   const float inv = none ? 0.f : f.v / total;
   if (a.mask) {

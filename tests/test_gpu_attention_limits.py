@@ -68,3 +68,15 @@ def test_rows_that_see_nothing_beside_non_finite_numbers(dtype, value, what, m, 
             want, S = clean[name]
             assert torch.isfinite(got[name]).all(), name
             assert ((got[name] - want).abs() <= tol * S + 2.0 ** -25).all(), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [3, 90])
+def test_rows_whose_bias_is_minus_infinity_beside_non_finite_values(dtype, m):
+    """Without a mask: all scores of a head are -inf, and V holds Inf."""
+    case = Case(dtype, heads=2, m=m, k=150, d=32, buckets=8, span=16, seed=9)
+    case.table[0] = -float("inf")
+    case.V[0, 0, 70] = float("inf")
+    got = step(case)
+    assert (got["O"][0, 0] == 0).all() and torch.isneginf(got["lse"][0, 0]).all() and (got["dQ"][0, 0] == 0).all()
+    assert all(torch.isfinite(got[name][0, 1]).all() for name in ("O", "lse", "dQ", "dK", "dV"))
