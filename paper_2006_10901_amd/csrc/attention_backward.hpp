@@ -627,6 +627,11 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     }
   }
 
+  // states behind the sequence's last: the weights of 0 that their lanes have times Inf or NaN of Q, dO or D are NaN
+  if (!valid) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) dk[b] = dv[b] = f32x16{};
+  }
   const float offset = __builtin_amdgcn_exp2f(-kOffset);
   const float to_dk = a.scale * f.q * offset / ds_scale.factor, to_dv = f.g * offset;
   const bool stored = key < a.k;

@@ -3,7 +3,7 @@ see nothing and behind a sequence's states, numbers of unequal size in one head.
 import pytest
 import torch
 
-from tests.attention_util import Case, reference, sparse_rows
+from tests.attention_util import Case, causal, reference, sparse_rows
 from tests.gpu_util import TOL_F16, TOL_F32
 
 pytestmark = pytest.mark.gpu
@@ -80,3 +80,21 @@ def test_rows_whose_bias_is_minus_infinity_beside_non_finite_values(dtype, m):
     got = step(case)
     assert (got["O"][0, 0] == 0).all() and torch.isneginf(got["lse"][0, 0]).all() and (got["dQ"][0, 0] == 0).all()
     assert all(torch.isfinite(got[name][0, 1]).all() for name in ("O", "lse", "dQ", "dK", "dV"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("what", ["Q", "dO"])
+@pytest.mark.parametrize("mask", [None, causal], ids=["all", "causal"])
+@pytest.mark.parametrize("m,k,heads", [(50, 150, 2), (2050, 150, 1), (3, 150, 2)])
+def test_gradients_behind_the_states_beside_non_finite_numbers(dtype, value, what, mask, m, k, heads):
+    """What stands in Q and dO reaches no state that the sequence does not have: its gradients are 0."""
+    lengths = [37, 150, 1, 0, 65]
+    case = Case(dtype, batch=5, heads=heads, kv_heads=1, m=m, k=k, d=40, lengths=lengths, mask=mask, seed=m)
+    getattr(case, what)[:, 0, m // 2] = value
+    got = step(case)
+    for b, n in enumerate(lengths):
+        for name in ("dK", "dV"):
+            assert (got[name][b, :, n:] == 0).all(), f"{name} of sequence {b}, behind {n} states"
+    hit = got["dK"][1, 0, 100] if mask is None else got["dQ"][1, 0, m // 2]      # (and it does reach those that are seen)
+    assert mask is not None or not torch.isfinite(hit).all()
