@@ -280,6 +280,8 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V; of K and V: in a head; of P and dS: in
  * a row or a block of rows).  In the _f16 ones weights P, and dS in the gradients, are rounded to binary16 (taken times a power of two
  * that keeps them in its range) before they are multiplied, and results are rounded once.  Two calls on the same inputs give the same bits.
+ * Scores may be of any size: those of rows whose lse (or its distance from the bias) is above 128 are taken relative to the row's largest before they are
+ * multiplied by log2 e, and their weights over their sum, in the gradients too (up to half as long again there).
  * Inf and NaN: a row that does not see a state, by its mask or the sequence's length, is not touched by what stands there, and neither
  * are gradients; with a mask, rows that such numbers would reach otherwise are formed again one position at a time, at the speed of
  * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.  A bias of -inf is no mask in this sense: the

@@ -29,7 +29,7 @@ struct Plan {
   // offsets into the workspace, in bytes; the terms of Q, K, V and dO and their factors come first (single precision)
   int64_t most, factors, q16, k16, v16, g16;
   int64_t forward_part, part_sum, forward_again, forward_bytes;
-  int64_t delta, weight, ends, part, row_sums, part_bias, backward_again, backward_bytes;
+  int64_t delta, weight, ends, top, large, part, row_sums, part_bias, backward_again, backward_bytes;
 };
 
 inline int kernel_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
@@ -110,6 +110,8 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   x.delta = take(end, x.rows);
   x.weight = take(end, x.rows);
   x.ends = take(end, 2 * x.rows);
+  x.top = take(end, x.rows);
+  x.large = take(end, x.dq_blocks * kAttnWaves);
   x.part = take(end, std::max(x.dq_splits > 1 ? x.dq_splits * x.rows * p.d : 0, x.dkv_splits > 1 ? 2 * x.dkv_splits * x.kv_rows * p.d : 0));
   if (x.dq_splits > 1) x.row_sums = take(end, 2 * x.dq_splits * x.rows * kAttnRowSums);
   if (p.buckets > 0) {
@@ -364,6 +366,8 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   a.delta = reinterpret_cast<float*>(w + x.delta);
   a.weight = reinterpret_cast<float*>(w + x.weight);
   a.ends = reinterpret_cast<float*>(w + x.ends);
+  a.top = reinterpret_cast<float*>(w + x.top);
+  a.large = reinterpret_cast<int*>(w + x.large);
   a.row_sums = reinterpret_cast<double*>(w + x.row_sums);
   a.part_bias = dtable ? reinterpret_cast<float*>(w + x.part_bias) : nullptr;
   const hipStream_t s = static_cast<hipStream_t>(stream);

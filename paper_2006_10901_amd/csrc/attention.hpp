@@ -57,6 +57,8 @@ struct AttnArgs {
   float* delta;          // workspace, of each row: D, what its weights are taken times, the sums of dS at the bias's ends
   float* weight;
   float* ends;
+  float* top;            // and what its P is relative to
+  int* large;            // and of each 32 rows of a head, from panel to panel: kLarge, kLargeLse
   float* part;           // workspace: what splits leave for the join
   float2* part_sum;      // and of each row its maximum and its sum relative to that (not lse: beside a maximum of 1e9 the sum would be lost)
   double* row_sums;      // workspace: of every split and row, the sums over its keys
@@ -273,23 +275,29 @@ template <int D, int TERMS> struct AttnOwn {
   }
 };
 
+// x += a piece of rows times one of own rows, 16 columns.  In single precision the smallest products first, in the same order whether the rows are
+// keys or (QUERIES) queries: a score then has the same bits wherever it is formed.
+template <bool QUERIES, int D, int TERMS>
+__device__ __forceinline__ void attn_multiply(f32x16& x, const AttnOwn<D, TERMS>& rows, const AttnOwn<D, TERMS>& own, int s) {
+  if constexpr (TERMS == 2) {
+    constexpr int kFirst = QUERIES ? 0 : 1;
+    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(rows.v[kFirst][s], own.v[1 - kFirst][s], x, 0, 0, 0);
+    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(rows.v[1 - kFirst][s], own.v[kFirst][s], x, 0, 0, 0);
+  }
+  x = __builtin_amdgcn_mfma_f32_32x32x16_f16(rows.v[0][s], own.v[0][s], x, 0, 0, 0);
+}
+
 // X += (32 rows of the tile) (own)^T
-template <int PITCH, int D, int TERMS>
+template <int PITCH, bool QUERIES = false, int D, int TERMS>
 __device__ __forceinline__ void attn_product(f32x16& x, const char* lds, const AttnOwn<D, TERMS>& own, int lane) {
   const char* row = lds + (lane & 31) * PITCH + (lane >> 5) * 16;
-  f16x8 a[TERMS][D / 16];
+  AttnOwn<D, TERMS> a;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-    for (int t = 0; t < TERMS; ++t) a[t][s] = *reinterpret_cast<const f16x8*>(row + t * D * 2 + s * 32);
+    for (int t = 0; t < TERMS; ++t) a.v[t][s] = *reinterpret_cast<const f16x8*>(row + t * D * 2 + s * 32);
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    if constexpr (TERMS == 2) {
-      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][s], own.v[0][s], x, 0, 0, 0);
-      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][s], own.v[1][s], x, 0, 0, 0);
-    }
-    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][s], own.v[0][s], x, 0, 0, 0);
-  }
+  for (int s = 0; s < D / 16; ++s) attn_multiply<QUERIES>(x, a, own, s);
   // the reads run ahead of the products by four, rather than each product waiting for its own
   constexpr int kReads = TERMS * D / 16, kAhead = kReads < 4 ? kReads : 4, kPer = TERMS == 2 ? 3 : 1;
   __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
@@ -518,9 +526,14 @@ __device__ __forceinline__ void attn_add_constant(f32x16& x, float scale, float 
 struct AttnRunning { float most = -__builtin_inff(), sum = 0.f; };
 
 // How the scores of a tile come from products: s = scale x + bias.  Where one bias goes for all of them (no bias, or a tile at one end of
-// it) it takes one instruction per score to be the exponent of a weight.  Where each has its own, or the one is so large that scores
-// are lost in it (and have to be, as in any sum of the two), the scores are formed first: three.
-constexpr float kAttnLargeBias = 1e6f;
+// it) it takes one instruction per score to be the exponent of a weight, 2^(c x + shift), two numbers that nearly cancel: each is rounded to
+// 2^-24 of itself, so that the weight of a score s (without its bias) is off by up to 2.6e-7 |s| of itself.  Where each score has its own bias, or the one
+// is so large that scores are lost in it (and have to be, as in any sum of the two), or scores are larger than kAttnLargeScore, they are formed
+// first and what they are relative to is subtracted from them: three.  (At 128 the short form costs 3.4e-5 of a weight, a fifteenth of what rounding it
+// to fp16 does; at 1e4 it would cost 0.2 %, at 2e7 weights would leave the range of fp16.)
+constexpr float kAttnLargeBias = 1e6f, kAttnLargeScore = 128.f;
+// Whether the difference of a bias and a row's largest score or lse calls for the long form (not that of a row without weights, whose lse is +inf).
+__device__ __forceinline__ bool attn_large(float v) { return fabsf(v) > kAttnLargeScore && attn_finite(v); }
 struct AttnScores { float scale; bool formed; float bias; };
 
 // x: NB blocks of products (AttnScores::formed: of scores).  Brings the running maximum up to date, scales what has been summed before,
@@ -546,7 +559,19 @@ __device__ __forceinline__ AttnExponent attn_softmax_step(f32x16 (&x)[NB], AttnR
     run.most = now;
   }
   const float base = run.most == -__builtin_inff() ? 0.f : run.most;
-  if (!how.formed) return {how.scale * kLog2e, __builtin_fmaf(how.bias - base, kLog2e, kOffset)};
+  if (!how.formed) {
+    float shift = __builtin_fmaf(how.bias - base, kLog2e, kOffset);
+    if (__any(attn_large(how.bias - base))) {
+      asm volatile("");
+      const float inv = 1.f / how.scale;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[b][r] = (__builtin_fmaf(x[b][r], how.scale, how.bias) - base) * inv;
+      shift = kOffset;
+    }
+    return {how.scale * kLog2e, shift};
+  }
   // subtracted first: a bias of the type's lowest value times log2 e would be an infinity
   asm volatile("");
 #pragma unroll
@@ -662,6 +687,9 @@ __device__ __forceinline__ float2 attn_exact_forward(const AttnArgs& a, int batc
 // The logarithm of a row's sum; that of a row that sees nothing: -inf.
 __device__ __forceinline__ float attn_lse(float2 s) { return s.y == 0.f ? -__builtin_inff() : s.x + __builtin_amdgcn_logf(s.y) * kLn2; }
 
+// The weight of a score that lies `above` what it is relative to: by no more than rounding (a score added up in another order), but of 1e9 that is 64 and more.
+__device__ __forceinline__ float attn_exact_weight(float above) { return __builtin_amdgcn_exp2f((above > 0.f ? fminf(above, 1.f) : above) * kLog2e); }
+
 // dQ of one row over the keys [begin, end).  weight: what P is taken times.
 template <typename T, typename OUT>
 __device__ __forceinline__ void attn_exact_dq(const AttnArgs& a, int batch, int head, int row, int begin, int end, float lse, float delta, float weight,
@@ -673,7 +701,7 @@ __device__ __forceinline__ void attn_exact_dq(const AttnArgs& a, int batch, int 
   AttnLane out = {0.f, 0.f};
   attn_each_seen(a.mask ? a.mask + lay.row_words : nullptr, lay.ti * 64, row, begin, end, [&](int key) {
     const AttnLane k = attn_lane_row(attn_row<T>(a.K, a.kk, batch, kv_head, key), a.d, lane);
-    const float p = weight * __builtin_amdgcn_exp2f((attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse) * kLog2e);
+    const float p = weight * attn_exact_weight(attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse);
     const float ds = p * (attn_lane_dot(g, attn_lane_row(attn_row<T>(a.V, a.v, batch, kv_head, key), a.d, lane)) - delta);
     out.a = __builtin_fmaf(ds, k.a, out.a);
     out.b = __builtin_fmaf(ds, k.b, out.b);
@@ -697,12 +725,11 @@ __device__ __forceinline__ void attn_exact_dkv(const AttnArgs& a, int batch, int
     if (from >= to) continue;
     attn_each_seen(a.mask ? a.mask + lay.col_words : nullptr, lay.tj * 64, key, (int)from * 64, min((int)to * 64, a.m), [&](int row) {
       const int64_t flat = ((int64_t)batch * a.heads + head) * a.m + row;
-      const float lse = a.lse[flat];
+      const float lse = a.top[flat];
       if (lse == -__builtin_inff()) return;
       const AttnLane q = attn_lane_row(attn_row<T>(a.Q, a.q, batch, head, row), a.d, lane);
       const AttnLane g = attn_lane_row(attn_row<T>(a.dO, a.dout, batch, head, row), a.d, lane);
-      float p = __builtin_amdgcn_exp2f((attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse) * kLog2e);
-      if (sizeof(T) == 4) p *= a.weight[flat];
+      const float p = a.weight[flat] * attn_exact_weight(attn_score<T>(a, batch, head, row, key, attn_lane_dot(q, k)) - lse);
       const float ds = p * (attn_lane_dot(g, v) - a.delta[flat]);
       dk.a = __builtin_fmaf(ds, q.a, dk.a), dk.b = __builtin_fmaf(ds, q.b, dk.b);
       dv.a = __builtin_fmaf(p, g.a, dv.a), dv.b = __builtin_fmaf(p, g.b, dv.b);

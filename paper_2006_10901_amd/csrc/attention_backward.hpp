@@ -45,26 +45,26 @@ __device__ __forceinline__ bool attn_far(int near, int span) { return near - 31 
 
 // What a pass over a row's keys tells of the row: the sums of dS and of P over all of them and, for the gradient of the bias, over the
 // blocks that lie at its lower and at its upper end (half precision: of P only there).  Added up in 64 bits: sums of thousands of terms that nearly cancel.
+// `top`: what P is relative to, lse or (where lse is large, see attn_row_top) the largest score of those keys.
 //
-// P comes from lse, which is rounded to 2^-24 of itself: an error of up to 5e-7 that all weights of a row share.  D is off by
+// P comes from lse, which is rounded to 2^-24 of itself: an error of up to 5e-7 (at an lse of 8) that all weights of a row share.  D is off by
 // what rounding O cost.  But P adds up to 1 over a row, and dS to 0, so that the sums tell both errors: weights are P / sum P, and D
 // is right once sum dS / sum P is added.  (Single precision: 9.2e-7 -> 4.7e-7 of dK's 2-norm.  Half precision with a bias: dtable's sums
 // nearly cancel and were off by 3.8e-4 .. 1.2e-3, now 1.7e-4, what rounding the result costs.)
 struct AttnRowSums { double ds, p, low, low_p, high, high_p; };
-constexpr int kAttnRowSums = 6;
-// Whether a call needs them, and the weights' part of it.
+constexpr int kAttnRowSums = 7;                           // with the top
+// Whether a call needs them for all rows.
 template <typename T, bool BIAS> constexpr bool attn_row_sums() { return BIAS || sizeof(T) == 4; }
 
-// (half precision takes sum P as 1; a row of Inf or NaN keeps its weights and its D)
-template <typename T> __device__ __forceinline__ double attn_row_weight(const AttnRowSums& s) {
-  return sizeof(T) == 4 && s.p > 0. && s.p < 1e30 ? 1. / s.p : 1.;
-}
-// What the other kernels take of a row: D, 1 / sum P (single precision) and the sums of dS at the ends.
-template <typename T, bool BIAS>
-__device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat, float delta, const AttnRowSums& s) {
-  const double weight = attn_row_weight<T>(s), more = s.ds * weight;
+// (a row of Inf or NaN keeps its weights and its D)
+__device__ __forceinline__ double attn_row_weight(double sum_p) { return sum_p > 0. && sum_p < 1e30 ? 1. / sum_p : 1.; }
+// What the other kernels take of a row: D, what P is relative to, 1 / sum P and the sums of dS at the ends.
+template <bool BIAS>
+__device__ __forceinline__ void attn_finish_row(const AttnArgs& a, int64_t flat, float delta, const AttnRowSums& s, float top, double weight) {
+  const double more = s.ds * weight;
   a.delta[flat] = more == more ? (float)(delta + more) : delta;
-  if constexpr (sizeof(T) == 4) a.weight[flat] = (float)weight;
+  a.top[flat] = top;
+  a.weight[flat] = (float)weight;
   if constexpr (BIAS) {
     a.ends[2 * flat] = (float)(weight * (s.low - more * s.low_p));
     a.ends[2 * flat + 1] = (float)(weight * (s.high - more * s.high_p));
@@ -74,11 +74,11 @@ template <bool BIAS> __device__ __forceinline__ AttnRowSums attn_row_sums_of(con
   const int64_t rows = (int64_t)a.batch * a.heads * a.m;
   AttnRowSums s = {};
   for (int i0 = 0; i0 < a.splits; i0 += 4) {             // four parts asked for at a time, behind the last one that again
-    double v[4][kAttnRowSums];
+    double v[4][6];
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int x = 0; x < (BIAS ? kAttnRowSums : 2); ++x) v[u][x] = a.row_sums[(min(i0 + u, a.splits - 1) * rows + flat) * kAttnRowSums + x];
+      for (int x = 0; x < (BIAS ? 6 : 2); ++x) v[u][x] = a.row_sums[(min(i0 + u, a.splits - 1) * rows + flat) * kAttnRowSums + x];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (i0 + u >= a.splits) break;
@@ -89,25 +89,52 @@ template <bool BIAS> __device__ __forceinline__ AttnRowSums attn_row_sums_of(con
   return s;
 }
 
+// Of 32 rows: whether weights of any of them take the long form (AttnScores); and whether their lse is why.
+constexpr int kLarge = 1, kLargeLse = 2;
+
 // A workgroup's panel of queries for the backward pass.
 template <typename T, int D, bool BIAS> struct AttnQueries {
   static constexpr int kTerms = attn_terms<T>();
   AttnOwn<D, kTerms> q, g;
   float scale, lse, to_dp;
+  bool large, large_lse;                                 // as kLarge, kLargeLse
   int64_t flat;
-  __device__ __forceinline__ void load(const AttnArgs& a, const AttnPanelOf& at, const AttnFactors& f, int row, bool valid, int half) {
+  // lse_of: lse, or each row's top
+  __device__ __forceinline__ void load(const AttnArgs& a, const AttnPanelOf& at, const AttnFactors& f, const float* lse_of, int row, bool valid, int half) {
     flat = ((int64_t)at.batch * a.heads + at.head) * a.m + row;
     q.load(a.q16 + at.batch * a.q16s.batch + at.head * a.q16s.head, row * a.q16s.row, valid, a.width, half);
     g.load(a.g16 + at.batch * a.g16s.batch + at.head * a.g16s.head, row * a.g16s.row, valid, a.width, half);
     if (a.scale < 0.f) q.negate();
     scale = fmaxf(fabsf(a.scale) * (f.q * f.k), kAttnLeastScale);
     to_dp = f.g * f.v;
-    lse = valid ? a.lse[flat] : -__builtin_inff();
+    lse = valid ? lse_of[flat] : -__builtin_inff();
     if (lse == -__builtin_inff()) lse = __builtin_inff();  // rows that see nothing, and those behind the last, have no weights
+    large = large_lse = __any(attn_large(lse));
+    if constexpr (BIAS) {
+      // the bias's two ends
+      const T* table = static_cast<const T*>(a.table) + (int64_t)at.head * a.buckets;
+      const int first = a.bucket_of[0], last = a.bucket_of[2 * a.span];
+      const float low = (float)table[min(max(first, 0), a.buckets - 1)], high = (float)table[min(max(last, 0), a.buckets - 1)];
+      large |= !(fabsf(low) < kAttnLargeBias && fabsf(high) < kAttnLargeBias) || __any(attn_large(low - lse) || attn_large(high - lse));
+    }
   }
-  // Products become weights, with one bias for all of them (AttnScores), or each with its own
+  // Products become weights: without a bias, with one for all of them, or each with its own
+  __device__ __forceinline__ void weights(f32x16& x) const {
+    float shift = -lse * kLog2e;
+    if (large) {
+      // in place, as products that come to the same in the short form without a shift (a branch around both forms costs the registers of one of them)
+      asm volatile("");
+      const float inv = 1.f / scale;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = (__builtin_fmaf(x[r], scale, 0.f) - lse) * inv;
+      shift = 0.f;
+    }
+    const float c = scale * kLog2e;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shift));
+  }
   __device__ __forceinline__ void weights(f32x16& x, float bias) const {
-    if (fabsf(bias) < kAttnLargeBias) {
+    if (!large) {
       const float c = scale * kLog2e, shift = (bias - lse) * kLog2e;
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shift));
@@ -121,6 +148,55 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
     for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f((__builtin_fmaf(x[r], scale, bias[8 * (r / 4) + r % 4]) - lse) * kLog2e);
   }
 };
+
+// Where lse is large, its rounding and that of the scores, which the forward pass may have added up in another order, are too: an lse of 1e9 is a multiple of 64.
+// The scores are then taken relative to the largest that the backward pass itself forms (a product has the same bits wherever it does) among the
+// keys [begin, end), and weights over their sum.  A pass of its own over K, from memory, for the few calls that need it: in the kernel's own
+// pass its registers would cost all others 12 %.
+template <typename T, int D, bool BIAS>
+__device__ __forceinline__ float2 attn_row_top(const AttnArgs& a, const AttnQueries<T, D, BIAS>& own, const AttnPanelOf& at, const _Float16* K, int row,
+                                               bool valid, int begin, int end, int lane) {
+  constexpr int kTerms = attn_terms<T>();
+  const int half = lane >> 5;
+  const MaskLayout lay(a.m, a.k);
+  const int position = BIAS ? attn_position(a, at.batch) : 0;
+  float top = -__builtin_inff(), sum = 0.f;
+  for (int key0 = begin; key0 < end; key0 += 32) {
+    const uint64_t word = attn_word(a.mask ? a.mask + lay.row_words + (int64_t)(key0 >> 6) * lay.ti * 64 : nullptr, row, valid);
+    const unsigned w = ((unsigned)(word >> (key0 & 32)) & attn_low_bits(end - key0)) >> (4 * half);
+    if (!__any(w != 0)) continue;
+    AttnOwn<D, kTerms> k;
+    k.load(K, min(key0 + (lane & 31), end - 1) * a.k16s.row, true, a.width, half);
+    f32x16 x = {};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) attn_multiply<false>(x, k, own.q, s);
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float bias = 0.f;
+      if (BIAS) {
+        const int rel = key0 + 8 * (r / 4) + 4 * half + r % 4 - position - row;
+        const int b = a.bucket_of[min(max(rel, -a.span), a.span) + a.span];
+        bias = (float)static_cast<const T*>(a.table)[(int64_t)at.head * a.buckets + min(max(b, 0), a.buckets - 1)];
+      }
+      x[r] = attn_select(w, r, __builtin_fmaf(x[r], own.scale, bias), -__builtin_inff());
+      most = fmaxf(most, x[r]);
+    }
+    const float now = fmaxf(top, attn_max_halves(most));
+    if (now == -__builtin_inff()) continue;
+    sum *= top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((top - now) * kLog2e);
+    top = now;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((x[r] - top) * kLog2e);
+  }
+  return {top, attn_sum_halves(sum)};
+}
+
+// Whether a row's weights are relative to the largest score instead of lse.
+__device__ __forceinline__ bool attn_row_large(const AttnArgs& a, int batch, int head, int row) {
+  const int blocks = (a.m + kAttnPanel - 1) / kAttnPanel * kAttnWaves;
+  return a.large[((int64_t)batch * a.heads + head) * blocks + row / 32] & kLargeLse;
+}
 
 // dQ, by panels of 128 queries, and D = dO . O.
 //
@@ -147,7 +223,7 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
   const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
   AttnQueries<T, D, BIAS> own;
-  own.load(a, at, f, row, valid, half);
+  own.load(a, at, f, a.lse, row, valid, half);
   float delta = 0.f;
   if (valid) {
     constexpr int kPiece = 16 / sizeof(T);
@@ -183,11 +259,25 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
   // products become weights; whether the block lies at an end of the bias
   auto weigh = [&](f32x16& x, int near) {
     const bool far = BIAS && attn_far(near, a.span);
-    if (!BIAS) own.weights(x, 0.f);
+    if constexpr (!BIAS) own.weights(x);
     else if (far) own.weights(x, lds_bias[near > 0 ? 2 * a.span + kAttnPadBlock : kAttnPadBlock]);
     else own.weights(x, lds_bias + kAttnPadBlock + a.span + near - (lane & 31) + 4 * half);
     return far;
   };
+  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
+  double* row_sums = a.row_sums + (at.split * rows + own.flat) * kAttnRowSums;      // where there are splits
+  if (at.split == 0 && lane == 0) a.large[(((int64_t)batch * a.heads + head) * at.panels + at.panel) * kAttnWaves + wave] = own.large_lse ? kLargeLse : own.large ? kLarge : 0;
+  if (own.large_lse) {
+    asm volatile("");
+    const float2 top = attn_row_top<T, D, BIAS>(a, own, at, K, row, valid, begin * kAttnTile, min(end * kAttnTile, seen), lane);
+    // (rows of Inf or NaN keep what they have, those that see none of these keys need none; lanes of a row store the same)
+    if (attn_finite(own.lse) && attn_finite(top.x)) own.lse = top.x;
+    if (valid && kTerms == 1) {
+      if (a.splits == 1) a.weight[own.flat] = (float)attn_row_weight(top.y);
+      else row_sums[1] = top.y;
+    }
+    if (valid && a.splits > 1) row_sums[6] = top.x;
+  }
   float to_ds = own.to_dp, delta_ds = delta, from_ds = 1.f;   // what makes dS, taken times the factor of ds_scale
 
   f32x16 acc[D / 32] = {};
@@ -289,32 +379,29 @@ __global__ __launch_bounds__(256, (attn_queries_each<T, D>())) void attention_dq
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) acc[b] = f32x16{};
   }
-  float weight = 1.f;                                    // what the row's P is taken times
-  const int64_t rows = (int64_t)a.batch * a.heads * a.m;
+  double weight = 1.;                                    // what the row's P is taken times
+  double s[6] = {sums.ds, sums.p, sums.low, sums.low_p, sums.high, sums.high_p};
   if constexpr (kSums) {
-    double s[kAttnRowSums] = {sums.ds, sums.p, sums.low, sums.low_p, sums.high, sums.high_p};
 #pragma unroll
-    for (int i = 0; i < kAttnRowSums; ++i) s[i] += __shfl_xor(s[i], 32);
-    const AttnRowSums all = {s[0], s[1], s[2], s[3], s[4], s[5]};
-    if (a.splits == 1) {
-      weight = (float)attn_row_weight<T>(all);
-      if (valid && half == 0) attn_finish_row<T, BIAS>(a, own.flat, delta, all);
-    } else if (valid && half == 0) {
-      if (tells) a.delta[own.flat] = delta;
-      double* to = a.row_sums + (at.split * rows + own.flat) * kAttnRowSums;
+    for (int i = 0; i < 6; ++i) s[i] += __shfl_xor(s[i], 32);
+  }
+  const AttnRowSums all = {s[0], s[1], s[2], s[3], s[4], s[5]};
+  if (a.splits == 1) {
+    if (kTerms == 2) weight = attn_row_weight(all.p);
+    else if (own.large_lse && valid) weight = a.weight[own.flat];
+    if (valid && half == 0) attn_finish_row<BIAS>(a, own.flat, delta, all, none ? -__builtin_inff() : own.lse, weight);
+  } else if (valid && half == 0) {
+    if (tells) a.delta[own.flat] = delta;
 #pragma unroll
-      for (int i = 0; i < kAttnRowSums; ++i)
-        if (BIAS || i < 2) to[i] = s[i];
-    }
-  } else if (valid && half == 0 && tells) {
-    a.delta[own.flat] = delta;
+    for (int i = 0; i < 6; ++i)
+      if ((BIAS || i < 2) && !(kTerms == 1 && i == 1 && own.large_lse)) row_sums[i] = s[i];
   }
   if (a.mask) {
     // (rows whose own numbers are Inf or NaN are right as they are, and so are those that see nothing)
     const unsigned bad = attn_not_finite(acc, false) & (unsigned)__ballot(valid && attn_finite(own.lse) && attn_finite(delta));
     if (lane == 0) a.again[blockIdx.x * kAttnWaves + wave] = bad;
   }
-  const float factor = weight * a.scale * f.k / ds_scale.factor;
+  const float factor = (float)weight * a.scale * f.k / ds_scale.factor;
   if (a.splits == 1) {
     T* dQ = static_cast<T*>(a.dQ) + batch * a.dq.batch + head * a.dq.head + (int64_t)row * a.dq.row;
     attn_store_rows<T, D>(dQ, valid, acc, factor, a.d, half);
@@ -335,7 +422,9 @@ __global__ __launch_bounds__(256) void attention_dq_again_kernel(const AttnArgs 
   for (; left; left &= left - 1) {
     const int row = at.panel * kAttnPanel + wave * 32 + __builtin_ctz(left);
     const int64_t flat = ((int64_t)at.batch * a.heads + at.head) * a.m + row;
-    const float lse = a.lse[flat], delta = a.delta[flat], weight = a.splits == 1 && sizeof(T) == 4 ? a.weight[flat] : 1.f;
+    const float delta = a.delta[flat], weight = a.splits == 1 ? a.weight[flat] : 1.f;
+    const float lse = a.splits == 1 ? a.top[flat] : attn_row_large(a, at.batch, at.head, row)
+                          ? (float)a.row_sums[((int64_t)at.split * a.batch * a.heads * a.m + flat) * kAttnRowSums + 6] : a.lse[flat];
     if (a.splits == 1)
       attn_exact_dq<T>(a, at.batch, at.head, row, begin * kAttnTile, min(end * kAttnTile, seen), lse, delta, weight,
                        static_cast<T*>(a.dQ) + at.batch * a.dq.batch + at.head * a.dq.head + (int64_t)row * a.dq.row, lane);
@@ -397,7 +486,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   const _Float16* V = a.v16 + batch * a.v16s.batch + kv_head * a.v16s.head;
   const AttnFactors f = attn_factors<T>(a, batch, kv_head);
   AttnQueries<T, D, true> own;
-  own.load(a, at, f, row, valid, half);
+  own.load(a, at, f, a.top, row, valid, half);
   attn_fill_bias<T, kAttnPadBlock>(lds_bias, a, head, tid, 256);
   float* sums = lds_sums + wave * n;
   float* block = lds_blocks + wave * kAttnDiagonalBlock;
@@ -408,7 +497,7 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
   double low = 0., high = 0.;
   if (valid) {
     delta = a.delta[own.flat];
-    if (sizeof(T) == 4) weight = a.weight[own.flat];
+    weight = a.weight[own.flat];
     if (half == 0 && at.split == 0) low = a.ends[2 * own.flat], high = a.ends[2 * own.flat + 1];
   }
 
@@ -470,25 +559,17 @@ __device__ __forceinline__ void attn_dbias(const AttnArgs& a, char* lds_raw) {
 }
 
 // dK and dV, by panels of 128 keys: a wave has 32 of them, tiles of 64 queries, of every head that shares the keys, are shared by the waves.
-// Two workgroups to a compute unit as for dQ (fp32, 64 columns 369 -> 292 us, fp16 96 106 -> 98), but not at 128 columns (fp16 143 -> 235).
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_kernel(const AttnArgs a) {
+// LARGE: all weights in the long form (AttnScores), and taken over their rows' sums in half precision as well.
+template <typename T, int D, bool BIAS, bool LARGE>
+__device__ __forceinline__ void attn_dkv(const AttnArgs& a, char* lds_raw, int split, int panel, int batch, int kv_head) {
   constexpr int kTerms = attn_terms<T>();
+  constexpr bool kWeights = kTerms == 2 || LARGE;
   using Tile = AttnTile<D, kTerms, attn_keys_each<T, D>()>;
-  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
-  if (BIAS && (int)blockIdx.x >= a.bias_from) {
-    attn_dbias<T, D>(a, lds_raw);
-    return;
-  }
   float* lds_stats = reinterpret_cast<float*>(lds_raw + Tile::kSets * Tile::kPair);     // of each set, 64 times: lse (as an exponent of 2; with
-  // a bias lse itself, and the exponents with the bias's two ends), D, what P is taken times
+  // a bias lse itself), D, what P is taken times, and the exponents with the bias's two ends
   float* lds_bias = lds_stats + Tile::kSets * 5 * kAttnTile;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = uniform(tid >> 6);
-  const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
-  const AttnPlace place(a, panels * a.splits, blockIdx.x, BIAS ? a.bias_from : gridDim.x);
-  const int split = place.piece % a.splits, panel = place.piece / a.splits, batch = place.batch, kv_head = place.kv_head;
-
   const int seen = attn_seen(a, batch);
   const int first_key = panel * kAttnPanel, wave_key = first_key + wave * 32, key = wave_key + (lane & 31);
   const bool valid = key < seen;
@@ -528,6 +609,8 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
   f32x16 dk[D / 32] = {}, dv[D / 32] = {};
   AttnScale ds_scale;
   typename Tile::template Stage<kAttnTile, 256> stage_q, stage_g;
+  // (one address for a wave: chosen lane by lane in the loop it was itself loaded, and waited for, in every tile: 98 -> 94 us)
+  const float* stats_of = (wave == 0 ? LARGE ? a.top : a.lse : wave == 1 ? a.delta : a.weight) + stat0;
   float stat = 0.f;
   const auto whole_q = stage_q.whole_offsets(a.q16s.row, tid);
   const auto whole_g = stage_g.whole_offsets(a.g16s.row, tid);
@@ -537,9 +620,7 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     word_next = attn_word(a.mask ? a.mask + lay.col_words + (int64_t)t * lay.tj * 64 : nullptr, key, valid);
     stage_q.load(Q + h * a.q16s.head + (int64_t)t * kAttnTile * a.q16s.row, a.q16s.row, rows, a.width, whole_q, tid);
     stage_g.load(dO + h * a.g16s.head + (int64_t)t * kAttnTile * a.g16s.row, a.g16s.row, rows, a.width, whole_g, tid);
-    const int r = tid & 63;
-    if (tid < (kTerms == 2 ? 192 : 128))
-      stat = r < rows ? (tid < 64 ? a.lse : tid < 128 ? a.delta : a.weight)[stat0 + (int64_t)h * a.m + t * kAttnTile + r] : tid < 64 ? -__builtin_inff() : 0.f;
+    if (wave < (kWeights ? 3 : 2)) stat = lane < rows ? stats_of[(int64_t)h * a.m + t * kAttnTile + lane] : wave == 0 ? -__builtin_inff() : 0.f;
   };
   bool more = next();
   int bias_head = -1;
@@ -567,12 +648,12 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     if (tid < 64) {
       // rows that see nothing, and those behind the last, have no weights
       const float l = stat == -__builtin_inff() ? __builtin_inff() : stat;
-      lds_lse[tid] = BIAS ? l : kOffset - l * kLog2e;
+      lds_lse[tid] = BIAS || LARGE ? l : kOffset - l * kLog2e;
       if (BIAS) {
         lds_ends[tid] = __builtin_fmaf(low - l, kLog2e, kOffset);
         lds_ends[64 + tid] = __builtin_fmaf(high - l, kLog2e, kOffset);
       }
-    } else if (tid < (kTerms == 2 ? 192 : 128)) {
+    } else if (tid < (kWeights ? 192 : 128)) {
       lds_lse[tid] = stat;
     }
     __syncthreads();
@@ -585,11 +666,10 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     for (int b = 0; b < 2; ++b) {
       const int near = wave_key - (position + row0 + 32 * b);
       f32x16 x = {}, y = {};
-      attn_product<Tile::kPitch>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
+      attn_product<Tile::kPitch, true>(x, lds_q + b * 32 * Tile::kPitch, kf, lane);
       attn_product<Tile::kPitch>(y, lds_g + b * 32 * Tile::kPitch, vf, lane);
       __builtin_amdgcn_s_setprio(1);                       // as in the forward pass (fp32 202 -> 194 us)
-      const bool far = BIAS && attn_far(near, a.span) && fabsf(near > 0 ? high : low) < kAttnLargeBias;
-      if (!BIAS || far) {
+      if (!LARGE && (!BIAS || attn_far(near, a.span))) {
         const float* shifts = (BIAS ? lds_ends + (near > 0 ? 64 : 0) : lds_lse) + b * 32 + half * 4;
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, shifts[8 * (r / 4) + r % 4]));
@@ -599,11 +679,11 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
         const float* l = lds_lse + b * 32 + half * 4;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float bias = lds_bias[kAttnPadBlock + min(max(rel - (8 * (r / 4) + r % 4), 0), 2 * a.span)];
+          const float bias = BIAS ? lds_bias[kAttnPadBlock + min(max(rel - (8 * (r / 4) + r % 4), 0), 2 * a.span)] : 0.f;
           x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(x[r], scale, bias) - l[8 * (r / 4) + r % 4], kLog2e, kOffset));
         }
       }
-      if constexpr (kTerms == 2) {
+      if constexpr (kWeights) {
         const float* weights = lds_weight + b * 32 + half * 4;
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] *= weights[8 * (r / 4) + r % 4];
@@ -649,6 +729,25 @@ __global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_k
     attn_store_rows<float, D>(a.part + (split * rows + flat) * a.d, stored, dk, to_dk, a.d, half);
     attn_store_rows<float, D>(a.part + ((a.splits + split) * rows + flat) * a.d, stored, dv, to_dv, a.d, half);
   }
+}
+// Two workgroups to a compute unit as for dQ (fp32, 64 columns 369 -> 292 us, fp16 96 106 -> 98), but not at 128 columns (fp16 143 -> 235).
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(256, (attn_keys_each<T, D>())) void attention_dkv_kernel(const AttnArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  if (BIAS && (int)blockIdx.x >= a.bias_from) {
+    attn_dbias<T, D>(a, lds_raw);
+    return;
+  }
+  const int panels = (a.k + kAttnPanel - 1) / kAttnPanel;
+  const AttnPlace place(a, panels * a.splits, blockIdx.x, BIAS ? a.bias_from : gridDim.x);
+  // One answer for all rows of the heads, and two copies of the kernel: with a branch in each block the short form takes longer
+  // (fp16, us: 64 columns, 8 x 16 heads of 512 x 2048 94 -> 98, 96 and 128 columns, 2 x 8 heads of 2048 x 2048 68 -> 73 and 122 -> 126).
+  const int blocks = a.group * ((a.m + kAttnPanel - 1) / kAttnPanel) * kAttnWaves, *of = a.large + ((int64_t)place.batch * a.kv_heads + place.kv_head) * blocks;
+  int any = 0;
+  for (int i = threadIdx.x & 63; i < blocks; i += 64) any |= of[i];
+  const int split = place.piece % a.splits, panel = place.piece / a.splits;
+  if (__builtin_expect(__any(any), 0)) attn_dkv<T, D, BIAS, true>(a, lds_raw, split, panel, place.batch, place.kv_head);
+  else attn_dkv<T, D, BIAS, false>(a, lds_raw, split, panel, place.batch, place.kv_head);
 }
 template <typename T>
 __global__ __launch_bounds__(256) void attention_dkv_again_kernel(const AttnArgs a) {
@@ -702,13 +801,46 @@ __global__ __launch_bounds__(256) void attention_sum_dq_kernel(const AttnArgs a)
   if (at >= rows * pieces) return;
   const int64_t flat = at / pieces;
   const bool first = at % pieces == 0;
+  const int c = (int)(at % pieces) * 4, i = (int)(flat % a.m);
+  const int64_t bh = flat / a.m;
+  if (attn_row_large(a, (int)(bh / a.heads), (int)(bh % a.heads), i)) {
+    // parts relative to the largest score of each
+    auto sum_of = [&](int s, int x) { return a.row_sums[(s * rows + flat) * kAttnRowSums + x]; };
+    // (that of NaN stays as it is: its parts have no scale)
+    const float lse = a.lse[flat];
+    float top = -__builtin_inff();
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, (float)sum_of(s, 6));
+    const bool scaled = attn_finite(lse) && attn_finite(top);
+    AttnRowSums all = {};
+    f32x4 value = {};
+    for (int s = 0; s < a.splits; ++s) {
+      const float own = (float)sum_of(s, 6);
+      const double factor = !scaled ? 1. : own == -__builtin_inff() ? 0. : (double)__builtin_amdgcn_exp2f((own - top) * kLog2e);
+      if (factor == 0.) continue;
+      value += (float)factor * attn_load_piece<float>(a.part + (s * rows + flat) * a.d, c, a.d);
+      all.p += factor * sum_of(s, 1);
+      if (SUMS) all.ds += factor * sum_of(s, 0);
+      if (BIAS) all.low += factor * sum_of(s, 2), all.low_p += factor * sum_of(s, 3), all.high += factor * sum_of(s, 4), all.high_p += factor * sum_of(s, 5);
+    }
+    const double w = attn_row_weight(all.p);
+    if (first) attn_finish_row<BIAS>(a, flat, a.delta[flat], all, scaled ? top : lse, w);
+    T* row = static_cast<T*>(a.dQ) + bh / a.heads * a.dq.batch + bh % a.heads * a.dq.head + (int64_t)i * a.dq.row;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < a.d) row[c + e] = (T)(value[e] * (float)w);
+    return;
+  }
   float weight = 1.f;
   if (SUMS && (sizeof(T) == 4 || first)) {
     const AttnRowSums s = attn_row_sums_of<BIAS>(a, flat);
-    weight = (float)attn_row_weight<T>(s);
-    if (first) attn_finish_row<T, BIAS>(a, flat, a.delta[flat], s);
+    const double w = sizeof(T) == 4 ? attn_row_weight(s.p) : 1.;
+    weight = (float)w;
+    if (first) attn_finish_row<BIAS>(a, flat, a.delta[flat], s, a.lse[flat], w);
+  } else if (first) {
+    a.top[flat] = a.lse[flat];
+    a.weight[flat] = 1.f;
   }
-  attn_add_parts<T>(a.splits, rows, a.heads, a.m, a.d, a.part, flat, (int)(at % pieces) * 4, weight, AttnSum{a.dq, a.dQ});
+  attn_add_parts<T>(a.splits, rows, a.heads, a.m, a.d, a.part, flat, c, weight, AttnSum{a.dq, a.dQ});
 }
 
 // dtable of one head: the panels' sums by relative position (runs of panels by as many groups of threads as 1024 allow, added up in their

@@ -1,5 +1,7 @@
 """Attention where numbers, lengths and masks meet the ends of what they may be: large biases and scores, Inf and NaN beside rows that
 see nothing and behind a sequence's states, numbers of unequal size in one head."""
+import math
+
 import pytest
 import torch
 
@@ -98,3 +100,92 @@ def test_gradients_behind_the_states_beside_non_finite_numbers(dtype, value, wha
             assert (got[name][b, :, n:] == 0).all(), f"{name} of sequence {b}, behind {n} states"
     hit = got["dK"][1, 0, 100] if mask is None else got["dQ"][1, 0, m // 2]      # (and it does reach those that are seen)
     assert mask is not None or not torch.isfinite(hit).all()
+
+
+def close(got, want, allowed, dtype, what):
+    """Results of half precision that may be above its largest number, 65504, may be Inf."""
+    beyond = (want.abs() + allowed > 65504) & (dtype == "f16")
+    assert torch.isfinite(got[~beyond]).all() and not torch.isnan(got).any(), what
+    off = torch.where(beyond, 0.0, (got - want).abs() - allowed)
+    assert (off <= 0).all(), f"{what}: {off.max():.2e} more than allowed"
+
+
+def pairs(dtype, m, k, d, score, bias=None, heads=2, seed=0):
+    """States in pairs of equal K: each row's score is about `score` (and its bias) for both of one pair; the products of the others have random signs and
+    add up to less than 0.6 of that.  P is 1/2 twice and 0 else by the definition.  Fp32 and fp16 numbers of any last bits."""
+    case = Case(dtype, heads=heads, m=m, k=k, d=d, seed=seed, buckets=4 if bias is not None else 0, span=3)
+    gen = torch.Generator().manual_seed(seed)
+    half = (k + 1) // 2
+    K = (torch.randint(0, 2, (1, heads, half, d), generator=gen) * 2 - 1) * (0.5 + 0.5 * torch.rand((1, heads, half, d), generator=gen))
+    chosen = torch.arange(m) * 7 % half
+    size = math.sqrt(score * math.sqrt(d) / (0.58 * d))  # the mean of squares of 0.5 .. 1 is 0.58
+    Q = K[:, :, chosen] * size
+    case.Q = Q.to(case.dt).cuda()
+    case.K = (K * size).to(case.dt).repeat_interleave(2, 2)[:, :, :k].contiguous().cuda()
+    if bias is not None:
+        case.table[:] = bias
+    return case
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("score", [1e3, 1e4, 1e5, 1e6, 1e7, 2e7, 1e8, 1e9, 1e10])
+@pytest.mark.parametrize("m,k,bias", [(3, 200, None), (70, 200, None), (70, 60, None), (70, 2050, None), (200, 200, 3.0), (70, 200, -3.0), (12, 130, 3.0)])
+def test_large_scores(dtype, score, m, k, bias):
+    """Scores are sums of 128 products of one sign, off by at most 130 2^-24 of themselves, and P depends on their differences from the row's
+    largest and from lse.  Equal states have equal products whatever is rounded, so that P is 1/2 to the last bits in the forward pass, and in the
+    gradients as well once weights are taken over their sum: TOL_F32, or 2^-11 each for P, dS and the result and for D (TOL_F16)."""
+    case = pairs(dtype, m, k, 128, score, bias, seed=m + k)
+    got = step(case)
+    want = reference(case.Q, case.K, case.V, case.scale, bucket_of=case.bucket_of, table=case.table, dO=case.dO)
+    lse = want["lse"][0]
+    assert (lse > 0.8 * score - 10).all()
+    assert ((got["lse"] - lse).abs() <= 131 * 2.0 ** -24 * lse.abs() + 1e-5).all()
+    tol = TOL_F16 if dtype == "f16" else TOL_F32
+    for name in ("O", "dQ", "dK", "dV"):
+        result, S = want[name]
+        close(got[name], result, tol * S + 2.0 ** -25, dtype, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("score", [1e3, 1e5, 1e8, 1e10])
+@pytest.mark.parametrize("m,k,heads,bias,poisoned", [(9, 200, 2, None, False), (70, 200, 2, None, False), (70, 2050, 1, 3.0, False), (200, 140, 16, None, False),
+                                                     (9, 200, 2, None, True), (70, 200, 2, None, True), (70, 2050, 1, 3.0, True)])
+def test_large_scores_with_a_mask(dtype, score, m, k, heads, bias, poisoned):
+    """As above, where rows see half of the states; poisoned: K and V of one that none sees are NaN, so that results are formed again one position at a
+    time.  A score then is added up in another order than the row's sum was, and may be off by 2 * 131 * 2^-24 of itself, all of the weight above 1e5."""
+    case = pairs(dtype, m, k, 128, score, bias, heads=heads, seed=m + k)
+    gen = torch.Generator().manual_seed(m)
+    case.seen = torch.rand((m, k), generator=gen) < 0.5
+    chosen = torch.arange(m) * 7 % ((k + 1) // 2)
+    for i in range(m):
+        case.seen[i, 2 * chosen[i]:2 * chosen[i] + 2] = True
+    if poisoned:
+        at = int((torch.bincount(chosen, minlength=k // 2)[:k // 2] == 0).nonzero()[-1]) * 2      # of a pair that no row has chosen
+        case.seen[:, at] = False
+    case.mask = case.build_mask()
+    want = reference(case.Q, case.K, case.V, case.scale, seen=case.seen, bucket_of=case.bucket_of, table=case.table, dO=case.dO)
+    if poisoned:
+        case.K[:, :, at] = case.V[:, :, at] = float("nan")
+    got = step(case)
+    tol = (TOL_F16 if dtype == "f16" else TOL_F32) + (math.expm1(min(1.0, 2 * 131 * 2.0 ** -24 * score)) if poisoned else 0.0)
+    for name in ("O", "dQ", "dK", "dV"):
+        result, S = want[name]
+        if poisoned and name in ("dK", "dV"):
+            assert (got[name][:, :, at] == 0).all(), name
+        close(got[name], result, tol * S + 2.0 ** -25, dtype, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,span", [(1, 150, 16), (40, 150, 16), (40, 150, 1000), (40, 2050, 16)])
+@pytest.mark.parametrize("entry", [-65504.0, 1234.5])
+def test_one_large_bias_for_all(dtype, m, k, span, entry):
+    """Scores of one large number only: P is 1 / k to a rounding whatever lse's own costs (2^-9 at 65504).  dV then is dO's sum over k, off by
+    2^-11 for P and 2^-11 for the result in half precision, and by TOL_F32 in single."""
+    case = Case(dtype, heads=2, m=m, k=k, d=64, buckets=8, span=span, seed=3)
+    case.Q.zero_()
+    case.table[:] = entry
+    got = step(case)
+    tol = 2 * 2.0 ** -11 + 1e-5 if dtype == "f16" else TOL_F32
+    dO = case.dO.cpu().double()
+    err, S = (got["dV"] - dO.sum(2, keepdim=True) / k).abs(), dO.abs().sum(2, keepdim=True) / k
+    assert (err <= tol * S + 2.0 ** -25).all(), f"{(err / S).max():.2e}"
