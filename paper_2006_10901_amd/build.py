@@ -50,8 +50,7 @@ CLOCKS_LIB_PATH = os.path.join(_HERE, "microbench", "libspdl_phase_clocks.so")
 def build_phase_clocks(verbose: bool = False) -> str:
     """A second copy of the library with clocks compiled into the slab kernels
     (-DSPDL_PHASE_CLOCKS), for microbench/phase_clocks.py only; the product library has none."""
-    return _compile_and_link(CLOCKS_LIB_PATH, ["-DSPDL_PHASE_CLOCKS"], [s for s in sources() if os.path.basename(s) not in SOURCE_FLAGS],
-                             verbose)
+    return _compile_and_link(CLOCKS_LIB_PATH, ["-DSPDL_PHASE_CLOCKS"], sources(), verbose)
 
 
 NATIVE_PATH = os.path.join(_HERE, "_native.so")
