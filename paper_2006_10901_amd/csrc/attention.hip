@@ -54,7 +54,8 @@ inline int split_count(int64_t blocks, int64_t steps, int each, int least, int f
   return (int)std::min<int64_t>(std::max<int64_t>(s, 1), 64);
 }
 
-Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
+// backward: of the strides of dO, which the forward pass does not take, the plan of that is to know nothing
+Plan make_plan(const spdl_attention_problem& p, int elem_bytes, bool backward) {
   Plan x{};
   const int64_t group = p.kv_heads ? p.heads / p.kv_heads : 1;
   x.rows = (int64_t)p.batch * p.heads * p.m;
@@ -87,7 +88,7 @@ Plan make_plan(const spdl_attention_problem& p, int elem_bytes) {
   x.most_parts = (int)std::max<int64_t>(1, std::min<int64_t>({64, up(std::max<int64_t>(group * p.m, p.k), 64), (1 << 16) / kv}));
 
   int64_t terms = 0, end = 0;
-  const int64_t longest = std::max(std::max(p.Q.row, p.K.row), std::max(p.V.row, p.dO.row));
+  const int64_t longest = std::max({p.Q.row, p.K.row, p.V.row, backward ? p.dO.row : 0});
   x.copied = elem_bytes == 4 || p.d % 8 != 0 || longest >= 1 << 24;
   const int numbers = elem_bytes == 4 ? x.width : x.width / 2;    // floats' room that a row of terms takes
   if (x.copied) {
@@ -323,7 +324,7 @@ int attention(const spdl_attention_problem* p, const void* Q, const void* K, con
   if (!output_strides_ok(p->O, p->batch, p->heads, p->m, p->d)) return SPDL_ERR_INVALID;
   if (p->batch == 0 || p->heads == 0 || p->m == 0) return SPDL_OK;
   if (!Q || !O || (p->k > 0 && (!K || !V))) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p, sizeof(T));
+  const Plan x = make_plan(*p, sizeof(T), false);
   if (!workspace_ok(workspace, workspace_bytes, x.forward_bytes)) return SPDL_ERR_INVALID;
   AttnArgs a = make_args(*p, Q, K, V, lengths, positions, mask, bucket_of, table, O, lse);
   a.splits = x.forward_splits;
@@ -358,7 +359,7 @@ int attention_backward(const spdl_attention_problem* p, const void* Q, const voi
   const bool queries = p->batch > 0 && p->m > 0, keys = p->batch > 0 && p->k > 0;
   if (queries && (!Q || !O || !lse || !dO || !dQ)) return SPDL_ERR_INVALID;
   if (keys && (!K || !V || !dK || !dV)) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p, sizeof(T));
+  const Plan x = make_plan(*p, sizeof(T), true);
   if ((queries || keys) && !workspace_ok(workspace, workspace_bytes, x.backward_bytes)) return SPDL_ERR_INVALID;
   AttnArgs a = make_args(*p, Q, K, V, lengths, positions, mask, bucket_of, table, const_cast<void*>(O), const_cast<float*>(lse));
   a.dO = dO, a.dQ = dQ, a.dK = dK, a.dV = dV;
@@ -382,8 +383,8 @@ extern "C" {
 
 int64_t spdl_attention_workspace(const spdl_attention_problem* p, int elem_bytes, int backward) {
   if (!p || !sizes_ok(*p) || p->d > kMostWidth || (elem_bytes != 2 && elem_bytes != 4)) return SPDL_ERR_INVALID;
-  const Plan x = make_plan(*p, elem_bytes);
-  return backward ? std::max(x.forward_bytes, x.backward_bytes) : x.forward_bytes;
+  const int64_t forward = make_plan(*p, elem_bytes, false).forward_bytes;
+  return backward ? std::max(forward, make_plan(*p, elem_bytes, true).backward_bytes) : forward;
 }
 
 int spdl_attention(const spdl_attention_problem* problem, const float* Q, const float* K, const float* V, const int* lengths,
