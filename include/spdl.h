@@ -259,7 +259,7 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  *   lse[b,h,i] = log sum_j exp(s_ij),   P_ij = exp(s_ij - lse[b,h,i]),   O[b,h,i,:] = sum_j P_ij V[b,g,j,:]
  * with g = h / (heads / kv_heads): consecutive query heads share a head of K and V.  A row that sees nothing, or whose scores are all
  * -inf, has O = 0, lse = -inf and no part in any gradient.
- *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads), 1 <= d <= 128
+ *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads: with none of one there is none of the other), 1 <= d <= 128
  *     (SPDL_ERR_UNSUPPORTED above); batch*heads <= 2^21, batch*heads*ceil(max(m, k) / 128) < 2^23.  scale: finite.
  *     span (0 .. 1024) and buckets (1 .. 128) are those of the bias.
  *     Strides, in elements, of [batch, head, row] for each tensor; the d elements of a row lie next to one another.  Those of inputs

@@ -142,7 +142,7 @@ bool output_strides_ok(const spdl_strides& s, int64_t batch, int64_t heads, int6
 
 bool sizes_ok(const spdl_attention_problem& p) {
   if (p.batch < 0 || p.heads < 0 || p.kv_heads < 0 || p.m < 0 || p.k < 0 || p.d < 1 || p.m > kMostRows || p.k > kMostRows) return false;
-  if (p.heads > 0 && (p.kv_heads < 1 || p.heads % p.kv_heads)) return false;
+  if ((p.heads == 0) != (p.kv_heads == 0) || (p.heads > 0 && p.heads % p.kv_heads)) return false;
   if (p.span < 0 || p.span > kAttnSpanMax || p.buckets < 0 || p.buckets > kAttnBucketsMax) return false;
   if (!std::isfinite(p.scale)) return false;
   // grids: of 256 threads to a workgroup, 2^32 in all; of single tokens there are at most heads (m / 4 + 1) workgroups to a sequence

@@ -1,6 +1,8 @@
 """Attention's host side at the ends of what a problem may say."""
+import pytest
+
 import paper_2006_10901_amd as spdl
-from tests.test_attention_host import problem
+from tests.test_attention_host import INVALID, backward, forward, problem
 
 
 def test_the_forward_pass_does_not_look_at_the_strides_of_gradients():
@@ -14,3 +16,11 @@ def test_the_forward_pass_does_not_look_at_the_strides_of_gradients():
     # the backward pass takes copies of rows that far apart
     p = problem(m=300, k=5000)
     assert spdl.spdl_attention_workspace(problem(m=300, k=5000, dO=(2 ** 40, 2 ** 32, 2 ** 24)), 2, True) > spdl.spdl_attention_workspace(p, 2, True)
+
+
+def test_heads_of_k_and_v_that_no_query_head_shares_are_refused():
+    """Their gradients would have to be written, and there is nothing to write them."""
+    for p in (problem(heads=0, kv_heads=2), problem(heads=0, kv_heads=1, m=0), problem(heads=0, kv_heads=4, batch=0)):
+        assert forward(p) == INVALID and forward(p, f16=True) == INVALID and backward(p) == INVALID
+        with pytest.raises(spdl.SpdlError):
+            spdl.spdl_attention_workspace(p, 4, True)
