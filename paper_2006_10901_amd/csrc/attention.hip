@@ -221,8 +221,10 @@ bool prepare_operands(const Plan& x, AttnArgs& a, char* w, bool backward, hipStr
     if (hipGetLastError() != hipSuccess) return false;
   }
   if (rows == 0) return true;
+  // (a grid holds fewer than 2^32 threads one way: the workgroups of a long operand take more than one block of rows)
   const int64_t blocks = up(rows, 256 / (D / 8));
-  attention_terms_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)std::min<int64_t>(each, 32768)), dim3(256), 0, stream>>>(o, (int)each);
+  attention_terms_kernel<T, D><<<dim3((unsigned)std::min<int64_t>(blocks, 1 << 16), (unsigned)std::min<int64_t>(each, 32768)), dim3(256), 0, stream>>>(
+      o, blocks, (int)each);
   return hipGetLastError() == hipSuccess;
 }
 

@@ -776,24 +776,16 @@ __global__ __launch_bounds__(256) void attention_largest_kernel(const AttnOperan
 // Copies of the operands for the panel kernels, rows of D numbers, zeros behind d and behind a sequence's states.  Single precision:
 // numbers times the power of two as two fp16 terms, the first ones of a row before the second ones.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands o, int each) {
+__global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands o, int64_t blocks, int each) {
   constexpr int kPieces = D / 8, kRows = 256 / kPieces;
   for (int id = blockIdx.y; id < each; id += gridDim.y) {
-    const int64_t block = blockIdx.x;
     const int which = id % o.count;
     const int64_t bh = id / o.count;
     const int kv_head = (int)(bh % o.kv_heads), batch = (int)(bh / o.kv_heads);
     const AttnOperand& x = o.of[which];
     const int64_t all = (int64_t)x.group * x.rows, rows = attn_operand_rows(o, x, batch);
-    const int64_t r = block * kRows + threadIdx.x / kPieces;
-    const bool mine = r < all && threadIdx.x < kRows * kPieces;
-    const int c = threadIdx.x % kPieces * 8;
-    _Float16* to = x.to + (bh * all + r) * (attn_terms<T>() * D) + c;
-    if constexpr (sizeof(T) == 2) {
-      f16x8 v = {};
-      if (mine && r < rows) v = attn_load_piece<_Float16>(attn_operand_row<_Float16>(x, batch, kv_head, r), c, o.d);
-      if (mine) *reinterpret_cast<f16x8*>(to) = v;
-    } else {
+    float factor = 1.f;
+    if constexpr (sizeof(T) == 4) {
       const int lane = threadIdx.x & 63;
       float most = 0.f;
       if (o.most) {
@@ -810,27 +802,39 @@ __global__ __launch_bounds__(256) void attention_terms_kernel(const AttnOperands
         most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
       }
       const int e = attn_exponent(most);
-      const float factor = ldexpf(1.f, e);
-      if (block == 0 && threadIdx.x == 0) o.factors[bh * 4 + o.first + which] = ldexpf(1.f, -e);
-      f16x8 hi = {}, lo = {};
-      if (mine && r < rows) {
-        const float* row = attn_operand_row<float>(x, batch, kv_head, r);
+      factor = ldexpf(1.f, e);
+      if (blockIdx.x == 0 && threadIdx.x == 0) o.factors[bh * 4 + o.first + which] = ldexpf(1.f, -e);
+    }
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+      const int64_t r = block * kRows + threadIdx.x / kPieces;
+      const bool mine = r < all && threadIdx.x < kRows * kPieces;
+      const int c = threadIdx.x % kPieces * 8;
+      _Float16* to = x.to + (bh * all + r) * (attn_terms<T>() * D) + c;
+      if constexpr (sizeof(T) == 2) {
+        f16x8 v = {};
+        if (mine && r < rows) v = attn_load_piece<_Float16>(attn_operand_row<_Float16>(x, batch, kv_head, r), c, o.d);
+        if (mine) *reinterpret_cast<f16x8*>(to) = v;
+      } else {
+        f16x8 hi = {}, lo = {};
+        if (mine && r < rows) {
+          const float* row = attn_operand_row<float>(x, batch, kv_head, r);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 v = attn_load_piece<float>(row, c + 4 * h, o.d) * factor;
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 v = attn_load_piece<float>(row, c + 4 * h, o.d) * factor;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            hi[4 * h + i] = (_Float16)v[i];
-            lo[4 * h + i] = (_Float16)(v[i] - (float)hi[4 * h + i]);
+            for (int i = 0; i < 4; ++i) {
+              hi[4 * h + i] = (_Float16)v[i];
+              lo[4 * h + i] = (_Float16)(v[i] - (float)hi[4 * h + i]);
+            }
           }
         }
+        if (mine) {
+          *reinterpret_cast<f16x8*>(to) = hi;
+          *reinterpret_cast<f16x8*>(to + D) = lo;
+        }
       }
-      if (mine) {
-        *reinterpret_cast<f16x8*>(to) = hi;
-        *reinterpret_cast<f16x8*>(to + D) = lo;
-      }
-      if (!o.most) __syncthreads();                       // `waves` is read
     }
+    if (sizeof(T) == 4 && !o.most) __syncthreads();       // `waves` is read
   }
 }
 

@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+import paper_2006_10901_amd as spdl
 from tests.attention_util import Case, causal, reference, sparse_rows
 from tests.gpu_util import TOL_F16, TOL_F32
 
@@ -189,3 +190,29 @@ def test_one_large_bias_for_all(dtype, m, k, span, entry):
     dO = case.dO.cpu().double()
     err, S = (got["dV"] - dO.sum(2, keepdim=True) / k).abs(), dO.abs().sum(2, keepdim=True) / k
     assert (err <= tol * S + 2.0 ** -25).all(), f"{(err / S).max():.2e}"
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 128), ("f16", 127)])
+def test_more_rows_than_one_round_of_workgroups_copies(dtype, d):
+    """A million states, whose terms (copies) take more blocks of rows than a grid has workgroups."""
+    k, m = 65536 * 16 + 100, 17
+    dt = torch.float16 if dtype == "f16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    Q, K, V = (torch.randn((1, 1, n, d), generator=gen, device="cuda").to(dt) for n in (m, k, k))
+    Q *= 2
+    K[0, 0, -1], V[0, 0, -1] = 3 * Q[0, 0, 3] / Q[0, 0, 3].norm() * 4, 100.0       # the last one is seen by some
+    O = torch.full_like(Q, float("nan"))
+    lse = torch.full((1, 1, m), float("nan"), device="cuda")
+    scale = 1 / math.sqrt(d)
+    p = spdl.attention_problem(Q, K, V, O, scale)
+    workspace = torch.empty(spdl.spdl_attention_workspace(p, K.element_size()), dtype=torch.uint8, device="cuda")
+    call = spdl.spdl_attention_f16 if dtype == "f16" else spdl.spdl_attention
+    call(p, Q, K, V, None, None, None, None, None, O, lse, workspace)
+    s = scale * (Q[0, 0].double() @ K[0, 0].double().T)
+    want = torch.logsumexp(s, 1)
+    P = torch.exp(s - want[:, None])
+    assert ((lse[0, 0] - want).abs() <= 1e-4).all()
+    S = P @ V[0, 0].double().abs()
+    assert ((O[0, 0].double() - P @ V[0, 0].double()).abs() <= (TOL_F16 if dtype == "f16" else TOL_F32) * S + 2.0 ** -25).all()
+    del Q, K, V, O, s, P, S, workspace
+    torch.cuda.empty_cache()
