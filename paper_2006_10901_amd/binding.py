@@ -302,8 +302,12 @@ def spdl_attention_mask_bytes(m, k):
 
 
 def spdl_build_attention_mask(m, k, nnz, row_offsets, column_indices, mask, stream=None):
-    if mask.numel() < spdl_attention_mask_bytes(m, k):
-        raise ValueError("mask is too short")
+    for name, t, n in (("mask", mask, spdl_attention_mask_bytes(m, k)), ("row_offsets", row_offsets, int(m) + 1 if nnz else 0),
+                       ("column_indices", column_indices, int(nnz))):
+        if getattr(t, "numel", None) is None:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if t.numel() < n:
+            raise ValueError(f"{name} is too short")
     _call["spdl_build_attention_mask"](m, k, nnz, row_offsets, column_indices, mask, stream)
     return mask
 
