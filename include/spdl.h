@@ -277,16 +277,19 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  *   workspace : DEVICE, spdl_attention_workspace bytes, 16-byte aligned; NULL where that is 0.  Its content before a call does not
  *     matter; calls that may run at the same time need one each.
  * Precision: all sums are fp32 or wider.  In the fp32 functions every factor of a product counts to 2^-23 of itself, or to 2^-39 of the
- * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V; of K and V: in a head; of P and dS: in
- * a row or a block of rows).  In the _f16 ones weights P, and dS in the gradients, are rounded to binary16 (taken times a power of two
- * that keeps them in its range) before they are multiplied, and results are rounded once.  Two calls on the same inputs give the same bits.
+ * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V, of Q in the forward pass in a row; of K and V: in a
+ * head; P: to 2^-39, in the forward pass of the row's largest; dS: to 2^-36 of the largest of 32 rows or states), and a product of two factors is off by up to another 2^-22 of itself
+ * (the product of their smaller halves, which is left out).  Single tokens (m <= 16, forward) are plain fp32 products.  In the _f16 functions weights P,
+ * and dS in the gradients, are rounded to binary16 (taken times a power of two that keeps them in its range) before they are multiplied, D is dO . O of
+ * the rounded O where a row's states do not lie in one tile of 64, and results are rounded once.  Two calls on the same inputs give the same bits.
  * Scores may be of any size: those of rows whose lse (or its distance from the bias) is above 128 are taken relative to the row's largest before they are
  * multiplied by log2 e, and their weights over their sum, in the gradients too (up to half as long again there).
  * Inf and NaN: a row that does not see a state, by its mask or the sequence's length, is not touched by what stands there, and neither
  * are gradients; with a mask, rows that such numbers would reach otherwise are formed again one position at a time, at the speed of
  * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.  A bias of -inf is no mask in this sense: the
  * weight of 0 that it gives, times Inf or NaN, may be NaN in O and in the gradients (a row all of whose scores are -inf still has O = 0 and dQ = 0).
- * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once.  */
+ * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once per 32 rows in fp16, in fp32
+ * once for up to 8 rows and once per 16 of more.  */
 typedef struct { int64_t batch, head, row; } spdl_strides;
 typedef struct {
   int batch, heads, kv_heads;

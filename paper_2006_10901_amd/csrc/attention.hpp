@@ -14,7 +14,7 @@
 //
 // Single precision: fp32 instructions do a sixteenth of the fp16 ones' work in the same time, so a number is two fp16 terms, taken times
 // a power of two that brings the largest of its head (all heads of a group) to 2^14 .. 2^15.  Two terms hold a number to 2^-23 of itself, or to
-// 2^-39 of the largest if that is more.  Of the four products of terms the smallest, below 2^-22 of the whole, is left out.
+// 2^-39 of the largest if that is more.  Of the four products of terms the smallest, at most 2^-22 of the whole, is left out.
 // The terms are made once per call, by two small kernels, rather than by every workgroup that reads them; those of Q in the forward pass,
 // which one workgroup reads, by that (8 sequences, 8 heads of 40 on two, 723 x 101: 31.9 -> 18.4 us; 8 heads of 128, 710 x 143: 63 -> 58).
 #pragma once

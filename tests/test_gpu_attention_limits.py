@@ -192,6 +192,33 @@ def test_one_large_bias_for_all(dtype, m, k, span, entry):
     assert (err <= tol * S + 2.0 ** -25).all(), f"{(err / S).max():.2e}"
 
 
+@pytest.mark.parametrize("m,k", [(3, 300), (40, 300), (200, 333)])
+def test_numbers_of_unequal_size_in_a_head(m, k):
+    """Rows of K, V, dO (and of Q in the second head that shares K and V) between 1 and 2^-20 of the largest, in single precision.  A factor
+    counts to 2^-23 of itself or to 2^-39 of the largest of its kind (dS: to 2^-36): beside what TOL_F32 allows, each sum may be off by those times what they meet."""
+    case = Case("f32", heads=2, kv_heads=1, m=m, k=k, d=64, seed=k)
+    gen = torch.Generator().manual_seed(k)
+    for t in (case.K, case.V, case.dO):
+        t.mul_((2.0 ** -torch.randint(0, 21, t.shape[:3], generator=gen).double()).float()[..., None].cuda())
+    case.Q[:, 1].mul_((2.0 ** -torch.randint(0, 21, case.Q.shape[2:3], generator=gen).double()).float()[:, None].cuda())
+    got = step(case)
+    want = reference(case.Q, case.K, case.V, case.scale, dO=case.dO)
+    Q, K, V, dO = (t.cpu().double() for t in (case.Q, case.K, case.V, case.dO))
+    most = lambda t: t.abs().max()
+    # P: of scores off by 64 products of 2^-39 of the largest factor, and what it counts to itself
+    p = 64 * case.scale * 2 * 2.0 ** -39 * most(Q) * most(K) + 2.0 ** -39
+    dp = 2 * (64 * 2 * 2.0 ** -39 * most(dO) * most(V))                   # of dP - D
+    # dS: P and dP as they are, and 2^-36 of the largest dS that a wave meets
+    ds = p * 2 * 64 * most(dO) * most(V) + dp + 2.0 ** -36 * 2 * 64 * most(dO) * most(V)
+    floor = {"O": p * V.abs().sum(2) + 2.0 ** -39 * most(V), "dV": (p * dO.abs().sum((1, 2)) + 2.0 ** -39 * 2 * m * most(dO))[None],
+             "dQ": case.scale * (ds * K.abs().sum(2) + k * 2.0 ** -39 * most(K) * 128 * most(dO) * most(V)),
+             "dK": case.scale * (ds * Q.abs().sum((1, 2)) + 2 * m * 2.0 ** -39 * most(Q) * 128 * most(dO) * most(V))[None]}
+    for name, more in floor.items():
+        result, S = want[name]
+        off = (got[name] - result).abs() - more[:, :, None, :]
+        assert (off <= TOL_F32 * S).all(), f"{name}: {off.max():.2e}"
+
+
 @pytest.mark.parametrize("dtype,d", [("f32", 128), ("f16", 127)])
 def test_more_rows_than_one_round_of_workgroups_copies(dtype, d):
     """A million states, whose terms (copies) take more blocks of rows than a grid has workgroups."""
