@@ -259,8 +259,8 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  *   lse[b,h,i] = log sum_j exp(s_ij),   P_ij = exp(s_ij - lse[b,h,i]),   O[b,h,i,:] = sum_j P_ij V[b,g,j,:]
  * with g = h / (heads / kv_heads): consecutive query heads share a head of K and V.  A row that sees nothing, or whose scores are all
  * -inf, has O = 0, lse = -inf and no part in any gradient.
- *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads: with none of one there is none of the other), 1 <= d <= 128
- *     (SPDL_ERR_UNSUPPORTED above); batch*heads <= 2^21, batch*heads*ceil(max(m, k) / 128) < 2^23.  scale: finite.
+ *   problem : HOST.  Sizes: batch, heads, kv_heads, m, k >= 0 (m, k <= 2^29; kv_heads divides heads: with none of one there is none of
+ *     the other), 1 <= d <= 128 (SPDL_ERR_UNSUPPORTED above); batch*heads <= 2^21, batch*heads*ceil(max(m, k) / 128) < 2^23.  scale: finite.
  *     span (0 .. 1024) and buckets (1 .. 128) are those of the bias.
  *     Strides, in elements, of [batch, head, row] for each tensor; the d elements of a row lie next to one another.  Those of inputs
  *     are >= 0 (0: the same for all); the elements of an output must not share addresses.  Only the strides of tensors that a
@@ -269,7 +269,7 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  *     may be NULL in the forward pass.  Base pointers are aligned to their element type; pieces of 16 bytes may start anywhere.
  *     Outputs and the workspace overlap neither one another nor an input.
  *   lengths : DEVICE int32[batch], how many states each sequence has (taken as 0 below 0, as k above k); NULL: k of each.  What lies
- *     in K and V behind a sequence's states is not read.
+ *     in K and V behind a sequence's states does not matter.
  *   mask : DEVICE, from spdl_build_attention_mask for this m and k; NULL: every position.  One for all sequences and heads.
  *   bucket_of : DEVICE int32[2*span+1], each in [0, buckets) (spdl_build_relative_buckets_host);  table : DEVICE [heads*buckets].
  *     Both NULL: no bias.  A bias of -inf gives a position the weight 0.
@@ -277,19 +277,21 @@ int spdl_validate_csr_host(int m, int k, int nnz, const int* row_offsets_host,
  *   workspace : DEVICE, spdl_attention_workspace bytes, 16-byte aligned; NULL where that is 0.  Its content before a call does not
  *     matter; calls that may run at the same time need one each.
  * Precision: all sums are fp32 or wider.  In the fp32 functions every factor of a product counts to 2^-23 of itself, or to 2^-39 of the
- * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V, of Q in the forward pass in a row; of K and V: in a
- * head; P: to 2^-39, in the forward pass of the row's largest; dS: to 2^-36 of the largest of 32 rows or states), and a product of two factors is off by up to another 2^-22 of itself
- * (the product of their smaller halves, which is left out).  Single tokens (m <= 16, forward) are plain fp32 products.  In the _f16 functions weights P,
- * and dS in the gradients, are rounded to binary16 (taken times a power of two that keeps them in its range) before they are multiplied, D is dO . O of
- * the rounded O where a row's states do not lie in one tile of 64, and results are rounded once.  Two calls on the same inputs give the same bits.
- * Scores may be of any size: those of rows whose lse (or its distance from the bias) is above 128 are taken relative to the row's largest before they are
- * multiplied by log2 e, and their weights over their sum, in the gradients too (up to half as long again there).
+ * largest of its kind if that is more (of Q and dO: in the heads that share one of K and V, of Q in the forward pass in a row; of K and
+ * V: in a head; P: to 2^-39, in the forward pass of the row's largest; dS: to 2^-36 of the largest of 32 rows or states), and a product of
+ * two factors is off by up to another 2^-22 of itself (the product of their smaller halves, which is left out).  Single tokens (m <= 16,
+ * forward) are plain fp32 products.  In the _f16 functions weights P, and dS in the gradients, are rounded to binary16 (taken times a
+ * power of two that keeps them in its range) before they are multiplied, D is dO . O of the rounded O where a row's states do not lie in
+ * one tile of 64, and results are rounded once.  Two calls on the same inputs give the same bits.
+ * Scores may be of any size: those of rows whose lse (or its distance from the bias) is above 128 are taken relative to the row's largest
+ * before they are multiplied by log2 e, and their weights over their sum, in the gradients too (up to half as long again there).
  * Inf and NaN: a row that does not see a state, by its mask or the sequence's length, is not touched by what stands there, and neither
  * are gradients; with a mask, rows that such numbers would reach otherwise are formed again one position at a time, at the speed of
- * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.  A bias of -inf is no mask in this sense: the
- * weight of 0 that it gives, times Inf or NaN, may be NaN in O and in the gradients (a row all of whose scores are -inf still has O = 0 and dQ = 0).
- * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once per 32 rows in fp16, in fp32
- * once for up to 8 rows and once per 16 of more.  */
+ * that.  What sees them comes out as Inf or NaN; where the formula gives Inf, NaN is possible.  A bias of -inf is no mask in this sense:
+ * the weight of 0 that it gives, times Inf or NaN, may be NaN in O and in the gradients (a row all of whose scores are -inf still has
+ * O = 0 and dQ = 0).
+ * m <= 16, a decoding step: rows of all query heads of a head of K and V are taken together, which are then read once per 32 rows in
+ * fp16, in fp32 once for up to 8 rows and once per 16 of more.  */
 typedef struct { int64_t batch, head, row; } spdl_strides;
 typedef struct {
   int batch, heads, kv_heads;

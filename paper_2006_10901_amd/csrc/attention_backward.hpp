@@ -149,10 +149,10 @@ template <typename T, int D, bool BIAS> struct AttnQueries {
   }
 };
 
-// Where lse is large, its rounding and that of the scores, which the forward pass may have added up in another order, are too: an lse of 1e9 is a multiple of 64.
-// The scores are then taken relative to the largest that the backward pass itself forms (a product has the same bits wherever it does) among the
-// keys [begin, end), and weights over their sum.  A pass of its own over K, from memory, for the few calls that need it: in the kernel's own
-// pass its registers would cost all others 12 %.
+// Where lse is large, its rounding and that of the scores, which the forward pass may have added up in another order, are too: an lse of
+// 1e9 is a multiple of 64.  The scores are then taken relative to the largest that the backward pass itself forms (a product has the same bits
+// wherever it does) among the keys [begin, end), and weights over their sum.  A pass of its own over K, from memory, for the few calls that
+// need it: in the kernel's own pass its registers would cost all others 12 % (fp16, 64 columns: 61 -> 69 us).
 template <typename T, int D, bool BIAS>
 __device__ __forceinline__ float2 attn_row_top(const AttnArgs& a, const AttnQueries<T, D, BIAS>& own, const AttnPanelOf& at, const _Float16* K, int row,
                                                bool valid, int begin, int end, int lane) {

@@ -152,8 +152,9 @@ def test_large_scores(dtype, score, m, k, bias):
 @pytest.mark.parametrize("m,k,heads,bias,poisoned", [(9, 200, 2, None, False), (70, 200, 2, None, False), (70, 2050, 1, 3.0, False), (200, 140, 16, None, False),
                                                      (9, 200, 2, None, True), (70, 200, 2, None, True), (70, 2050, 1, 3.0, True)])
 def test_large_scores_with_a_mask(dtype, score, m, k, heads, bias, poisoned):
-    """As above, where rows see half of the states; poisoned: K and V of one that none sees are NaN, so that results are formed again one position at a
-    time.  A score then is added up in another order than the row's sum was, and may be off by 2 * 131 * 2^-24 of itself, all of the weight above 1e5."""
+    """As above, where rows see half of the states; poisoned: K and V of one that none sees are NaN, so that results are formed again one
+    position at a time.  A score then is added up in another order than the row's sum was, and may be off by 2 * 131 * 2^-24 of itself,
+    all of the weight above 1e5."""
     case = pairs(dtype, m, k, 128, score, bias, heads=heads, seed=m + k)
     gen = torch.Generator().manual_seed(m)
     case.seen = torch.rand((m, k), generator=gen) < 0.5
@@ -194,8 +195,9 @@ def test_one_large_bias_for_all(dtype, m, k, span, entry):
 
 @pytest.mark.parametrize("m,k", [(3, 300), (40, 300), (200, 333)])
 def test_numbers_of_unequal_size_in_a_head(m, k):
-    """Rows of K, V, dO (and of Q in the second head that shares K and V) between 1 and 2^-20 of the largest, in single precision.  A factor
-    counts to 2^-23 of itself or to 2^-39 of the largest of its kind (dS: to 2^-36): beside what TOL_F32 allows, each sum may be off by those times what they meet."""
+    """Rows of K, V, dO (and of Q in the second head that shares K and V) between 1 and 2^-20 of the largest, in single precision.
+    A factor counts to 2^-23 of itself or to 2^-39 of the largest of its kind (dS: to 2^-36): beside what TOL_F32 allows, each sum may be off
+    by those times what they meet."""
     case = Case("f32", heads=2, kv_heads=1, m=m, k=k, d=64, seed=k)
     gen = torch.Generator().manual_seed(k)
     for t in (case.K, case.V, case.dO):
